@@ -410,6 +410,72 @@ tt_status tt_tree_rope(int64_t n_tokens, int32_t n_heads, int32_t d, int32_t dty
                        float theta_base, int32_t inverse, void* y, int64_t y_stride_tok, void* stream);
 
 /* ------------------------------------------------------------------------------------------
+ * tt_tree_logprob_entropy (device)
+ *
+ * The terms of a policy-gradient objective, per row r of the logits: lse_r = ln sum_v exp(z_rv),
+ * logp_r = z_r[target_r] - lse_r, entropy_r = -sum_v p_rv ln p_rv with p = softmax(z_r), and the top_k
+ * most probable entries.  The logits are read once.
+ *   logits, target as for tt_tree_weighted_logprob.  A row whose target is negative or >= vocab is
+ *     ignored: logp = 0 and entropy = 0, and its gradient is zero (lse and the alternatives are still
+ *     written).
+ *   top_k in [0, min(64, vocab)].  top_index, top_logp [n_rows][top_k]: indices in order of falling
+ *     log-prob, the lowest index first among equal logits, and their log-probs.  NaN counts as -inf.
+ *     Both NULL iff top_k == 0.
+ *   logp, entropy [n_rows] fp32, required; lse [n_rows] fp32 or NULL (the gradient needs it).
+ *   Entries at -inf have probability 0 and add nothing to the entropy; a row with a NaN, with an entry
+ *   at +inf or with nothing above -inf gives NaN.  Sums are fp32 and their order is fixed.
+ *   workspace: tt_tree_logprob_entropy_workspace bytes (few rows are worked on in parts), 16-byte
+ *     aligned; 0 from that function means that the sizes are invalid.
+ * Alignment: logits aligned to its element size.
+ *
+ * tt_tree_logprob_entropy_bwd: gradient of sum_r d_logp_r logp_r + d_entropy_r entropy_r,
+ *   dlogits[r][v] = d_logp_r ([v == target_r] - p_rv) - d_entropy_r p_rv (ln p_rv + entropy_r),
+ *   one read of the logits, one write (dtype of the logits, rounded to nearest even).  lse and entropy
+ *   are the forward's; d_logp, d_entropy [n_rows] fp32, each may be NULL (= 0).  Ignored rows get
+ *   exactly zero (their logits, lse and upstream gradients are not read).  dlogits may be logits when
+ *   the strides are equal; otherwise the two may not overlap.
+ * Alignment: both arrays aligned to the element size; where logits and gradient rows are the same
+ *   distance from a 16-byte boundary they go in vectors, otherwise element by element.
+ * ------------------------------------------------------------------------------------------ */
+#define TT_LOGPROB_TOP_MAX 64
+size_t tt_tree_logprob_entropy_workspace(int64_t n_rows, int32_t vocab, int32_t dtype, int32_t top_k);
+tt_status tt_tree_logprob_entropy(int64_t n_rows, int32_t vocab, int32_t dtype, const void* logits, int64_t row_stride,
+                                  const int32_t* target, int32_t top_k, float* logp, float* entropy, float* lse,
+                                  int32_t* top_index, float* top_logp, void* workspace, size_t workspace_bytes,
+                                  void* stream);
+tt_status tt_tree_logprob_entropy_bwd(int64_t n_rows, int32_t vocab, int32_t dtype, const void* logits,
+                                      int64_t row_stride, const int32_t* target, const float* lse,
+                                      const float* entropy, const float* d_logp, const float* d_entropy,
+                                      void* dlogits, int64_t dlogits_row_stride, void* stream);
+
+/* ------------------------------------------------------------------------------------------
+ * Rotary embedding with several position axes (device; host helper for the positions)
+ *
+ * tt_tree_rope_axes: tt_tree_rope with a position per axis (time, height, width of images and video).
+ * The pairs of a head share one ladder of frequencies, and each belongs to one axis:
+ *   angle_i = axis_pos[pair_axis[i]][t] * theta_base^(-2i/d),  i in [0, d/2)
+ * with the rotation of tt_tree_rope (rotate-half pairs, inverse, in place, dtypes, sizes, strides and
+ * alignment as there).
+ *   n_axes in 1..4; axis_pos [n_axes][n_tokens] int32 (device), any sign; pair_axis [d/2] (HOST, read
+ *   during the call), values below n_axes.  With equal positions on all axes the result is that of
+ *   tt_tree_rope.
+ *
+ * tt_tree_axis_positions (host only): positions [3][n_tokens] in DFS order for a tree of text and image
+ * nodes, Eq. 9 with three axes.  A node starts behind the largest position of its parent (a root at its
+ * root_pos_offset; NULL = 0).  Token i of a text node has start + i on all three axes.  A node with a
+ * grid of T x H x W tokens, row by row inside a frame, has start + (frame, row, column); it ends behind
+ * start + max(T, H, W) - 1.
+ *   grid [n_nodes][3] or NULL (all text): T, H, W of a node, 0 0 0 = text; T * H * W must be seg_len.
+ * Errors: TT_ERR_NULL, TT_ERR_SHAPE (a grid that does not match its node, positions past int32),
+ *   TT_ERR_TREE.
+ * ------------------------------------------------------------------------------------------ */
+tt_status tt_tree_rope_axes(int64_t n_tokens, int32_t n_heads, int32_t d, int32_t dtype, const void* x,
+                            int64_t x_stride_tok, int32_t n_axes, const int32_t* axis_pos, const uint8_t* pair_axis,
+                            float theta_base, int32_t inverse, void* y, int64_t y_stride_tok, void* stream);
+tt_status tt_tree_axis_positions(int32_t n_nodes, const int32_t* parent, const int32_t* seg_len, const int32_t* grid,
+                                 const int32_t* root_pos_offset, int32_t* axis_pos);
+
+/* ------------------------------------------------------------------------------------------
  * Tree-correct causal convolution (device; host helper for the backward)
  *
  * The depthwise causal conv1d in front of an SSM (GDN) layer, Section "Implementation", paragraph
@@ -642,7 +708,11 @@ tt_status tt_tree_gdn_bwd(int64_t n_tokens, int32_t hk, int32_t hv, int32_t dk, 
 #define TT_KERNEL_GDN_BWD_FSCAN  19  /* gated delta rule backward: forward walk that saves the states */
 #define TT_KERNEL_GDN_BWD_RSCAN  20  /* reverse walk (state gradients)                              */
 #define TT_KERNEL_GDN_BWD_FINISH 21  /* per-chunk gradients                                         */
-#define TT_N_KERNELS          22
+#define TT_KERNEL_ROPE_AXES      22  /* rotary embedding with several axes                           */
+#define TT_KERNEL_ENTROPY_ROWS   23  /* log-prob, entropy and alternatives, one pass over the logits */
+#define TT_KERNEL_ENTROPY_JOIN   24  /* parts of rows joined                                         */
+#define TT_KERNEL_ENTROPY_BWD    25  /* their gradient                                               */
+#define TT_N_KERNELS          26
 typedef struct {
   double  ms[TT_N_KERNELS];        /* summed kernel time in milliseconds */
   int64_t launches[TT_N_KERNELS];

@@ -8,4 +8,5 @@ from .binding import (  # noqa: F401
     kernel_timing_enable, kernel_timing_read, PartitionPlan, ConvPlan, GdnPlan, tree_gdn_plan, tree_gdn_fwd, tree_gdn_bwd, tree_gdn_bwd_workspace, GDN_CHUNK, tree_conv_plan, tree_conv_fwd, tree_conv_bwd, tree_conv_bwd_static, CONV_BWD_STATIC_SCRATCH_BYTES, tree_path_weights, WEIGHT_PATH_SUM, WEIGHT_UNIFORM, WEIGHT_PATH_TOKEN_MEAN,
     tree_partition_sizes, tree_partition_plan,
     tree_attn_partitioned_workspace, tree_attn_partitioned_fwd, tree_attn_partitioned_bwd,
+    tree_rope_axes, tree_axis_positions, LOGPROB_TOP_MAX, tree_logprob_entropy, tree_logprob_entropy_workspace, tree_logprob_entropy_bwd,
 )

@@ -1,6 +1,7 @@
 """ctypes binding of libtreetrain.so.  Argument marshalling only."""
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import os
 from dataclasses import dataclass
@@ -98,6 +99,19 @@ def _lib() -> ctypes.CDLL:
         lib.tt_tree_rope.restype = ctypes.c_int32
         lib.tt_tree_rope.argtypes = [ctypes.c_int64, ctypes.c_int32, ctypes.c_int32, ctypes.c_int32, _vp, ctypes.c_int64,
                                      _vp, ctypes.c_float, ctypes.c_int32, _vp, ctypes.c_int64, _vp]
+        lib.tt_tree_rope_axes.restype = ctypes.c_int32
+        lib.tt_tree_rope_axes.argtypes = [ctypes.c_int64, ctypes.c_int32, ctypes.c_int32, ctypes.c_int32, _vp, ctypes.c_int64,
+                                          ctypes.c_int32, _vp, ctypes.c_char_p, ctypes.c_float, ctypes.c_int32, _vp, ctypes.c_int64, _vp]
+        lib.tt_tree_axis_positions.restype = ctypes.c_int32
+        lib.tt_tree_axis_positions.argtypes = [ctypes.c_int32, _vp, _vp, _vp, _vp, _vp]
+        lib.tt_tree_logprob_entropy_workspace.restype = ctypes.c_size_t
+        lib.tt_tree_logprob_entropy_workspace.argtypes = [ctypes.c_int64, ctypes.c_int32, ctypes.c_int32, ctypes.c_int32]
+        lib.tt_tree_logprob_entropy.restype = ctypes.c_int32
+        lib.tt_tree_logprob_entropy.argtypes = [ctypes.c_int64, ctypes.c_int32, ctypes.c_int32, _vp, ctypes.c_int64, _vp, ctypes.c_int32,
+                                                _vp, _vp, _vp, _vp, _vp, _vp, ctypes.c_size_t, _vp]
+        lib.tt_tree_logprob_entropy_bwd.restype = ctypes.c_int32
+        lib.tt_tree_logprob_entropy_bwd.argtypes = [ctypes.c_int64, ctypes.c_int32, ctypes.c_int32, _vp, ctypes.c_int64, _vp, _vp, _vp,
+                                                    _vp, _vp, _vp, ctypes.c_int64, _vp]
         lib.tt_tree_conv_fwd.restype = ctypes.c_int32
         lib.tt_tree_conv_fwd.argtypes = [ctypes.c_int64, ctypes.c_int32, ctypes.c_int32, ctypes.c_int32, ctypes.c_int32, _vp,
                                          ctypes.c_int64, _vp, _vp, _vp, _vp, ctypes.c_int64, _vp]
@@ -159,7 +173,7 @@ def _lib() -> ctypes.CDLL:
 
 KERNEL_NAMES = ("attn_fwd", "loss_fused", "attn_dkdv", "attn_dq", "loss_rows", "loss_sum", "ref_fwd", "ref_bwd",
                 "attn_plan", "attn_reduce", "loss_bwd", "rope", "part_gather", "part_scatter", "conv_fwd", "conv_bwd", "conv_fix", "gdn_prepare", "gdn_scan",
-                "gdn_bwd_fscan", "gdn_bwd_rscan", "gdn_bwd_finish")
+                "gdn_bwd_fscan", "gdn_bwd_rscan", "gdn_bwd_finish", "rope_axes", "entropy_rows", "entropy_join", "entropy_bwd")
 
 
 class _KernelTimes(ctypes.Structure):
@@ -527,6 +541,40 @@ def _workspace(desc, backward, workspace, device):
     return workspace, workspace.numel() * workspace.element_size()
 
 
+def _check_tensor(t, name, shape, dtype):
+    """A contiguous tensor of exactly this shape and dtype."""
+    if tuple(t.shape) != tuple(shape) or t.dtype != dtype or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous {dtype} tensor of shape {tuple(shape)}")
+
+
+def _check_rows(t, name, shape, dtypes):
+    """Rows of contiguous elements with a free stride between them (one of the dtypes); returns that stride in elements."""
+    if tuple(t.shape) != tuple(shape) or t.dtype not in dtypes:
+        raise ValueError(f"{name} must be {tuple(shape)} of {' / '.join(str(d) for d in dtypes)}")
+    row = 1
+    for size, step in zip(t.shape[:0:-1], t.stride()[:0:-1]):
+        if size > 1 and step != row:
+            raise ValueError(f"the rows of {name} must be contiguous (only the stride between them is free)")
+        row *= size
+    if t.shape[0] <= 1:
+        return row
+    if t.stride(0) < row:
+        raise ValueError(f"the rows of {name} overlap")
+    return t.stride(0)
+
+
+def _launch_on(first, *others):
+    """Context in which a call on these tensors is made: their device, which must be one and the same GPU, is current."""
+    torch = _torch()
+    dev = first.device
+    if dev.type != "cuda":
+        raise ValueError("the tensors must be on the GPU")
+    for t in others:
+        if t is not None and t.device != dev:
+            raise ValueError(f"tensors on {dev} and {t.device} in one call")
+    return contextlib.nullcontext() if dev.index == torch.cuda.current_device() else torch.cuda.device(dev)
+
+
 def tree_attn_fwd(q, k, v, kend, kt_min, kt_max, *, k_prefix=None, v_prefix=None, scale=None,
                   o=None, lse=None, workspace=None, stream=None, reference_kernels: bool = False):
     """q [N,hq,d]; k, v [N,hkv,d]; kend/kt_min/kt_max: int32 device tensors from tree_build_meta.
@@ -612,6 +660,142 @@ def tree_rope(x, tok_pos, *, theta_base: float = 1.0e6, inverse: bool = False, o
     _check(_lib().tt_tree_rope(n, h, d, DTYPE_BF16 if x.dtype == torch.bfloat16 else DTYPE_FP32, _dp(x),
                                x.stride(0) if n > 1 else h * d, _dp(tok_pos), float(theta_base), 1 if inverse else 0,
                                _dp(out), out.stride(0) if n > 1 else h * d, _stream_ptr(stream)))
+    return out
+
+
+def _pair_axis(sections, n_axes: int, half: int, interleaved: bool) -> bytes:
+    sections = tuple(int(s) for s in sections)
+    if len(sections) != n_axes or min(sections) < 0 or sum(sections) != half:
+        raise ValueError(f"sections must hold one non-negative count per axis ({n_axes}), {half} pairs together")
+    if not interleaved:
+        return bytes(a for a, s in enumerate(sections) for _ in range(s))
+    return bytes(i % n_axes if i // n_axes < sections[i % n_axes] else 0 for i in range(half))
+
+
+def tree_rope_axes(x, axis_pos, sections, *, interleaved: bool = False, theta_base: float = 1.0e6, inverse: bool = False, out=None,
+                   stream=None):
+    """tree_rope with a position per axis (time, height, width): x [n, heads, d] bf16/fp32 (heads and d contiguous, free token
+    stride), axis_pos [n_axes, n] int32, 1 to 4 axes.  sections: pairs of every axis, d/2 together; the first axis has the first
+    pairs and so on or, interleaved, pair i belongs to axis i % n_axes while that axis has had fewer pairs than its section, and
+    to the first axis otherwise.  `inverse` undoes the rotation / is its backward; `out` may be x (in place)."""
+    torch = _torch()
+    if x.dim() != 3 or axis_pos.dim() != 2:
+        raise ValueError("x must be [tokens, heads, d], axis_pos [axes, tokens]")
+    n, h, d = x.shape
+    stride = _check_rows(x, "x", (n, h, d), (torch.bfloat16, torch.float32))
+    n_axes = axis_pos.shape[0]
+    _check_tensor(axis_pos, "axis_pos", (n_axes, n), torch.int32)
+    if not 1 <= n_axes <= 4:
+        raise ValueError("axis_pos must have 1 to 4 axes")
+    if d % 2:
+        raise ValueError("d must be even")
+    pair_axis = _pair_axis(sections, n_axes, d // 2, interleaved)
+    out_stride = h * d
+    if out is not None:
+        out_stride = _check_rows(out, "out", (n, h, d), (x.dtype,))
+    with _launch_on(x, axis_pos, out):
+        if out is None:
+            out = torch.empty((n, h, d), dtype=x.dtype, device=x.device)
+        _check(_lib().tt_tree_rope_axes(n, h, d, DTYPE_BF16 if x.dtype == torch.bfloat16 else DTYPE_FP32, _dp(x), stride, n_axes,
+                                        _dp(axis_pos), pair_axis, float(theta_base), 1 if inverse else 0, _dp(out), out_stride,
+                                        _stream_ptr(stream)))
+    return out
+
+
+def tree_axis_positions(parent, seg_len, grid=None, root_pos_offset=None) -> np.ndarray:
+    """Positions [3, n_tokens] (time, height, width) in DFS order of a tree of text and image nodes (host).  grid [n_nodes, 3]:
+    T, H, W of the nodes that hold images (T * H * W tokens, row by row inside a frame), zeros for text; a node starts behind the
+    largest position of its parent.  root_pos_offset: one entry per root, in ascending id."""
+    parent, seg_len = _np(parent, np.int32), _np(seg_len, np.int32)
+    if parent.shape != seg_len.shape or parent.ndim != 1:
+        raise ValueError("parent and seg_len must be 1-D arrays of equal length")
+    grid, root_pos_offset = _np(grid, np.int32), _np(root_pos_offset, np.int32)
+    if grid is not None and grid.shape != (len(parent), 3):
+        raise ValueError(f"grid must have shape ({len(parent)}, 3)")
+    sz = tree_meta_sizes(parent, seg_len)
+    if root_pos_offset is not None and root_pos_offset.shape != (sz["n_roots"],):
+        raise ValueError(f"root_pos_offset must have one entry per root ({sz['n_roots']})")
+    pos = np.zeros((3, sz["n_tokens"]), np.int32)
+    _check(_lib().tt_tree_axis_positions(len(parent), _hp(parent), _hp(seg_len), _hp(grid), _hp(root_pos_offset), _hp(pos)))
+    return pos
+
+
+LOGPROB_TOP_MAX = 64
+
+
+def _logits_dtype(logits) -> int:
+    torch = _torch()
+    if logits.dim() != 2:
+        raise ValueError("logits must be [rows, vocab]")
+    return DTYPE_BF16 if logits.dtype == torch.bfloat16 else DTYPE_FP32
+
+
+def tree_logprob_entropy_workspace(logits, top_k: int = 0) -> int:
+    """Bytes of workspace of tree_logprob_entropy for these logits."""
+    code, (n, vocab) = _logits_dtype(logits), logits.shape
+    need = int(_lib().tt_tree_logprob_entropy_workspace(n, vocab, code, int(top_k)))
+    if need == 0:
+        raise ValueError(f"top_k={top_k} must lie in [0, min({LOGPROB_TOP_MAX}, vocab={vocab})]")
+    return need
+
+
+def tree_logprob_entropy(logits, target, *, top_k: int = 0, logp=None, entropy=None, lse=None, top_index=None, top_logp=None,
+                         workspace=None, stream=None):
+    """Per row of the logits [n, V] (bf16/fp32, row stride free), in one pass: the log-prob of target [n] int32, the entropy of
+    the row's distribution, its log-sum-exp, and the top_k (at most 64) most probable entries.  Returns (logp [n], entropy [n],
+    lse [n] fp32, top_index [n, top_k] int32, top_logp [n, top_k] fp32), the last two None when top_k is 0: indices by falling
+    log-prob, the lowest index first among equals.  A row whose target lies outside [0, V) is ignored: logp and entropy are 0."""
+    torch = _torch()
+    code, (n, vocab) = _logits_dtype(logits), logits.shape
+    stride = _check_rows(logits, "logits", (n, vocab), (torch.bfloat16, torch.float32))
+    _check_tensor(target, "target", (n,), torch.int32)
+    top_k = int(top_k)
+    need = tree_logprob_entropy_workspace(logits, top_k) if n else 256
+    for name, t in (("logp", logp), ("entropy", entropy), ("lse", lse)):
+        if t is not None:
+            _check_tensor(t, name, (n,), torch.float32)
+    if top_k == 0 and (top_index is not None or top_logp is not None):
+        raise ValueError("top_index and top_logp need top_k > 0")
+    if top_index is not None:
+        _check_tensor(top_index, "top_index", (n, top_k), torch.int32)
+    if top_logp is not None:
+        _check_tensor(top_logp, "top_logp", (n, top_k), torch.float32)
+    with _launch_on(logits, target, logp, entropy, lse, top_index, top_logp, workspace):
+        dev = logits.device
+        new = lambda *shape, dtype=torch.float32: torch.empty(shape, dtype=dtype, device=dev)      # noqa: E731
+        logp, entropy, lse = (new(n) if t is None else t for t in (logp, entropy, lse))
+        if top_k:
+            top_index = new(n, top_k, dtype=torch.int32) if top_index is None else top_index
+            top_logp = new(n, top_k) if top_logp is None else top_logp
+        if workspace is None:
+            workspace = new(need, dtype=torch.uint8)
+        _check(_lib().tt_tree_logprob_entropy(n, vocab, code, _dp(logits), stride, _dp(target), top_k, _dp(logp), _dp(entropy),
+                                              _dp(lse), _dp(top_index), _dp(top_logp), _dp(workspace),
+                                              workspace.numel() * workspace.element_size(), _stream_ptr(stream)))
+    return logp, entropy, lse, top_index, top_logp
+
+
+def tree_logprob_entropy_bwd(logits, target, lse, entropy, d_logp=None, d_entropy=None, *, out=None, stream=None):
+    """Gradient of sum(d_logp * logp + d_entropy * entropy) with respect to the logits, in their dtype and shape; lse and entropy
+    [n] are the ones tree_logprob_entropy returned, d_logp and d_entropy [n] fp32 (None = 0).  Rows whose target lies outside
+    [0, V) get zero.  `out` may be the logits tensor itself (in place)."""
+    torch = _torch()
+    code, (n, vocab) = _logits_dtype(logits), logits.shape
+    stride = _check_rows(logits, "logits", (n, vocab), (torch.bfloat16, torch.float32))
+    _check_tensor(target, "target", (n,), torch.int32)
+    for name, t in (("lse", lse), ("entropy", entropy), ("d_logp", d_logp), ("d_entropy", d_entropy)):
+        if t is not None:
+            _check_tensor(t, name, (n,), torch.float32)
+        elif not name.startswith("d_"):
+            raise ValueError(f"{name} is required")
+    out_stride = vocab
+    if out is not None:
+        out_stride = _check_rows(out, "out", (n, vocab), (logits.dtype,))
+    with _launch_on(logits, target, lse, entropy, d_logp, d_entropy, out):
+        if out is None:
+            out = torch.empty((n, vocab), dtype=logits.dtype, device=logits.device)
+        _check(_lib().tt_tree_logprob_entropy_bwd(n, vocab, code, _dp(logits), stride, _dp(target), _dp(lse), _dp(entropy),
+                                                  _dp(d_logp), _dp(d_entropy), _dp(out), out_stride, _stream_ptr(stream)))
     return out
 
 

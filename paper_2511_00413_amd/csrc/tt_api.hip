@@ -254,6 +254,115 @@ extern "C" tt_status tt_tree_rope(int64_t n_tokens, int32_t n_heads, int32_t d, 
 }
 
 namespace {
+// Whether two arrays of `rows` rows of `len` bytes share memory.  Rows that interleave (slices of one buffer) do not; with unequal
+// steps the whole extents decide.
+bool shares_memory(const void* a, int64_t step_a, const void* b, int64_t step_b, int64_t len, int64_t rows) {
+  if (rows <= 0) return false;
+  const uintptr_t a0 = reinterpret_cast<uintptr_t>(a), b0 = reinterpret_cast<uintptr_t>(b);
+  if (step_a == step_b) {
+    const int64_t off = (int64_t)(b0 - a0), part = ((off % step_a) + step_a) % step_a, q = (off - part) / step_a;
+    // row i of b starts `part` bytes into row i + q of a
+    return (part < len && q > -rows && q < rows) || (step_a - part < len && q + 1 > -rows && q + 1 < rows);
+  }
+  const uintptr_t a1 = a0 + (uintptr_t)((rows - 1) * step_a + len), b1 = b0 + (uintptr_t)((rows - 1) * step_b + len);
+  return a0 < b1 && b0 < a1;
+}
+
+tt_status check_entropy(int64_t n_rows, int32_t vocab, int32_t dtype) {
+  if (dtype != TT_DTYPE_BF16 && dtype != TT_DTYPE_FP32) return fail(TT_ERR_DTYPE, "unknown dtype %d", dtype);
+  if (n_rows < 0 || n_rows > 0x7fffffffLL) return fail(TT_ERR_SHAPE, "n_rows=%lld out of range", (long long)n_rows);
+  if (vocab <= 0) return fail(TT_ERR_SHAPE, "vocab=%d must be positive", vocab);
+  return TT_OK;
+}
+tt_status check_top_k(int32_t vocab, int32_t top_k) {
+  if (top_k < 0 || top_k > TT_LOGPROB_TOP_MAX || top_k > vocab)
+    return fail(TT_ERR_SHAPE, "top_k=%d must lie in [0, min(%d, vocab=%d)]", top_k, TT_LOGPROB_TOP_MAX, vocab);
+  return TT_OK;
+}
+}  // namespace
+
+extern "C" size_t tt_tree_logprob_entropy_workspace(int64_t n_rows, int32_t vocab, int32_t dtype, int32_t top_k) {
+  tt::clear_error();
+  if (check_entropy(n_rows, vocab, dtype) || check_top_k(vocab, top_k)) return 0;
+  return tt::logprob_entropy_workspace(n_rows, vocab, dtype == TT_DTYPE_BF16, top_k);
+}
+
+extern "C" tt_status tt_tree_logprob_entropy(int64_t n_rows, int32_t vocab, int32_t dtype, const void* logits, int64_t row_stride,
+                                             const int32_t* target, int32_t top_k, float* logp, float* entropy, float* lse,
+                                             int32_t* top_index, float* top_logp, void* workspace, size_t workspace_bytes,
+                                             void* stream) {
+  tt::clear_error();
+  if (tt_status s = check_entropy(n_rows, vocab, dtype)) return s;
+  if (tt_status s = check_top_k(vocab, top_k)) return s;
+  if (row_stride == 0) row_stride = vocab;
+  if (row_stride < vocab) return fail(TT_ERR_SHAPE, "row_stride=%lld is smaller than vocab=%d", (long long)row_stride, vocab);
+  if (n_rows > 0 && (!logits || !target || !logp || !entropy)) return fail(TT_ERR_NULL, "logits / target / logp / entropy is NULL");
+  if (n_rows > 0 && ((top_k > 0) != (top_index != nullptr) || (top_k > 0) != (top_logp != nullptr)))
+    return fail(TT_ERR_NULL, "top_index and top_logp must be given exactly when top_k > 0");
+  const size_t es = dtype == TT_DTYPE_BF16 ? 2 : 4;
+  if (reinterpret_cast<uintptr_t>(logits) % es) return fail(TT_ERR_ALIGN, "logits is not aligned to its element size");
+  const size_t need = tt::logprob_entropy_workspace(n_rows, vocab, dtype == TT_DTYPE_BF16, top_k);
+  if (!workspace || workspace_bytes < need || !tt::aligned16(workspace))
+    return fail(TT_ERR_WORKSPACE, "tree_logprob_entropy needs %zu bytes of 16-byte aligned workspace, got %zu", need, workspace_bytes);
+  return hip_result(tt::logprob_entropy(n_rows, vocab, dtype == TT_DTYPE_BF16, logits, row_stride, target, top_k, logp, entropy, lse,
+                                        top_index, top_logp, workspace, (hipStream_t)stream),
+                    "tree_logprob_entropy");
+}
+
+extern "C" tt_status tt_tree_logprob_entropy_bwd(int64_t n_rows, int32_t vocab, int32_t dtype, const void* logits, int64_t row_stride,
+                                                 const int32_t* target, const float* lse, const float* entropy, const float* d_logp,
+                                                 const float* d_entropy, void* dlogits, int64_t dlogits_row_stride, void* stream) {
+  tt::clear_error();
+  if (tt_status s = check_entropy(n_rows, vocab, dtype)) return s;
+  if (row_stride == 0) row_stride = vocab;
+  if (dlogits_row_stride == 0) dlogits_row_stride = vocab;
+  if (row_stride < vocab || dlogits_row_stride < vocab)
+    return fail(TT_ERR_SHAPE, "row strides %lld / %lld are smaller than vocab=%d", (long long)row_stride, (long long)dlogits_row_stride,
+                vocab);
+  if (n_rows > 0 && (!logits || !target || !lse || !entropy || !dlogits))
+    return fail(TT_ERR_NULL, "logits / target / lse / entropy / dlogits is NULL");
+  const int64_t es = dtype == TT_DTYPE_BF16 ? 2 : 4;
+  if (reinterpret_cast<uintptr_t>(logits) % es || reinterpret_cast<uintptr_t>(dlogits) % es)
+    return fail(TT_ERR_ALIGN, "logits / dlogits is not aligned to its element size");
+  if (!(dlogits == logits && dlogits_row_stride == row_stride) &&
+      shares_memory(logits, row_stride * es, dlogits, dlogits_row_stride * es, vocab * es, n_rows))
+    return fail(TT_ERR_SHAPE, "dlogits may share memory with logits only as a whole, with equal row strides");
+  return hip_result(tt::logprob_entropy_bwd(n_rows, vocab, dtype == TT_DTYPE_BF16, logits, row_stride, target, lse, entropy, d_logp,
+                                            d_entropy, dlogits, dlogits_row_stride, (hipStream_t)stream),
+                    "tree_logprob_entropy_bwd");
+}
+
+extern "C" tt_status tt_tree_rope_axes(int64_t n_tokens, int32_t n_heads, int32_t d, int32_t dtype, const void* x, int64_t x_stride_tok,
+                                       int32_t n_axes, const int32_t* axis_pos, const uint8_t* pair_axis, float theta_base,
+                                       int32_t inverse, void* y, int64_t y_stride_tok, void* stream) {
+  tt::clear_error();
+  if (dtype != TT_DTYPE_BF16 && dtype != TT_DTYPE_FP32) return fail(TT_ERR_DTYPE, "unknown dtype %d", dtype);
+  if (n_tokens < 0 || n_tokens > 0x7fffffffLL) return fail(TT_ERR_SHAPE, "n_tokens=%lld out of range", (long long)n_tokens);
+  const int epv = dtype == TT_DTYPE_BF16 ? 8 : 4;
+  if (n_heads <= 0 || d <= 0 || d > 1024 || d % (2 * epv) != 0 || (int64_t)n_heads * d > 65536)
+    return fail(TT_ERR_SHAPE, "n_heads=%d, d=%d: d must be a multiple of %d in [%d, 1024] and n_heads * d <= 65536", n_heads, d,
+                2 * epv, 2 * epv);
+  if (!(theta_base > 1.f) || !std::isfinite(theta_base)) return fail(TT_ERR_SHAPE, "theta_base must be finite and > 1");
+  if (n_axes < 1 || n_axes > 4) return fail(TT_ERR_UNSUPPORTED, "n_axes=%d: 1 to 4 are built", n_axes);
+  if (!pair_axis) return fail(TT_ERR_NULL, "pair_axis is NULL");
+  for (int i = 0; i < d / 2; i++)
+    if (pair_axis[i] >= n_axes) return fail(TT_ERR_SHAPE, "pair_axis[%d]=%d with %d axes", i, pair_axis[i], n_axes);
+  if (x_stride_tok == 0) x_stride_tok = (int64_t)n_heads * d;
+  if (y_stride_tok == 0) y_stride_tok = (int64_t)n_heads * d;
+  if (x_stride_tok < (int64_t)n_heads * d || y_stride_tok < (int64_t)n_heads * d || x_stride_tok % epv || y_stride_tok % epv)
+    return fail(TT_ERR_SHAPE, "token strides %lld / %lld must be >= n_heads * d and a multiple of %d elements",
+                (long long)x_stride_tok, (long long)y_stride_tok, epv);
+  if (n_tokens > 0 && (!x || !y || !axis_pos)) return fail(TT_ERR_NULL, "x / y / axis_pos is NULL");
+  if (!tt::aligned16(x) || !tt::aligned16(y)) return fail(TT_ERR_ALIGN, "x / y is not 16-byte aligned");
+  const int64_t es = dtype == TT_DTYPE_BF16 ? 2 : 4, len = (int64_t)n_heads * d * es;
+  if (!(x == y && x_stride_tok == y_stride_tok) && shares_memory(x, x_stride_tok * es, y, y_stride_tok * es, len, n_tokens))
+    return fail(TT_ERR_SHAPE, "y may share memory with x only as a whole, with equal token strides");
+  return hip_result(tt::rope_axes(n_tokens, n_heads, d, dtype == TT_DTYPE_BF16, x, x_stride_tok, axis_pos, pair_axis, theta_base,
+                                  inverse != 0, y, y_stride_tok, (hipStream_t)stream),
+                    "tree_rope_axes");
+}
+
+namespace {
 
 struct ConvChecked { bool bf16; int64_t xs, ys; };
 

@@ -81,6 +81,19 @@ hipError_t weighted_logprob_fused(int64_t n_rows, int vocab, bool bf16, const vo
 hipError_t rope(int64_t n_tokens, int n_heads, int d, bool bf16, const void* x, int64_t x_stride, const int32_t* pos,
                 float theta_base, bool inverse, void* y, int64_t y_stride, hipStream_t st);
 
+// several position axes: axis_pos [n_axes][n_tokens] on the device, pair_axis [d / 2] (values < n_axes <= 4) on the host
+hipError_t rope_axes(int64_t n_tokens, int n_heads, int d, bool bf16, const void* x, int64_t x_stride, const int32_t* axis_pos,
+                     const uint8_t* pair_axis, float theta_base, bool inverse, void* y, int64_t y_stride, hipStream_t st);
+
+// log-prob of given tokens, entropy, most probable alternatives; gradient of the first two (tt_entropy.hip)
+size_t logprob_entropy_workspace(int64_t n_rows, int vocab, bool bf16, int top_k);
+hipError_t logprob_entropy(int64_t n_rows, int vocab, bool bf16, const void* logits, int64_t row_stride, const int32_t* target,
+                           int top_k, float* logp, float* entropy, float* lse, int32_t* top_index, float* top_logp, void* workspace,
+                           hipStream_t st);
+hipError_t logprob_entropy_bwd(int64_t n_rows, int vocab, bool bf16, const void* logits, int64_t row_stride, const int32_t* target,
+                               const float* lse, const float* entropy, const float* d_logp, const float* d_entropy, void* dlogits,
+                               int64_t out_stride, hipStream_t st);
+
 // tree-correct causal convolution (tt_conv.hip); strides in bytes
 hipError_t conv_fwd(int64_t n_tokens, int channels, int kernel_size, bool bf16, bool silu, const void* x, int64_t x_stride_bytes,
                     const float* weight, const float* bias, const int32_t* tok_pred, void* y, int64_t y_stride_bytes,

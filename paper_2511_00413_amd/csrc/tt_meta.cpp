@@ -189,6 +189,46 @@ extern "C" tt_status tt_tree_build_meta(int32_t n_nodes, const int32_t* parent, 
   return TT_OK;
 }
 
+extern "C" tt_status tt_tree_axis_positions(int32_t n_nodes, const int32_t* parent, const int32_t* seg_len, const int32_t* grid,
+                                            const int32_t* root_pos_offset, int32_t* axis_pos) {
+  tt::clear_error();
+  Forest f;
+  if (tt_status s = build_forest(n_nodes, parent, seg_len, 0, f)) return s;
+  if (f.n_tokens > 0 && !axis_pos) return tt::fail(TT_ERR_NULL, "axis_pos is NULL");
+  // where a node starts, and where what follows it starts; everything is checked before the first position is written
+  std::vector<int64_t> start(n_nodes), after(n_nodes);
+  int32_t root_no = 0;
+  for (int32_t rk = 0; rk < n_nodes; rk++) {
+    const int32_t i = f.order[rk];
+    start[i] = parent[i] < 0 ? (root_pos_offset ? root_pos_offset[root_no++] : 0) : after[parent[i]];
+    int64_t extent = seg_len[i];
+    if (grid) {
+      const int64_t T = grid[3 * i], H = grid[3 * i + 1], W = grid[3 * i + 2];
+      if (T || H || W) {
+        // (T * H is at most 2^62; divided rather than multiplied by W)
+        if (T <= 0 || H <= 0 || W <= 0 || seg_len[i] % W != 0 || T * H != seg_len[i] / W)
+          return tt::fail(TT_ERR_SHAPE, "node %d: a grid of %lld x %lld x %lld for %d tokens", i, (long long)T, (long long)H, (long long)W,
+                          seg_len[i]);
+        extent = std::max(T, std::max(H, W));
+      }
+    }
+    after[i] = start[i] + extent;
+    if (after[i] > INT32_MAX) return tt::fail(TT_ERR_SHAPE, "position id overflows int32 at node %d", i);
+  }
+  const int64_t N = f.n_tokens;
+  int64_t tok = 0;
+  for (int32_t rk = 0; rk < n_nodes; rk++) {
+    const int32_t i = f.order[rk], s = (int32_t)start[i];
+    const int32_t H = grid ? grid[3 * i + 1] : 0, W = grid ? grid[3 * i + 2] : 0;
+    for (int32_t k = 0; k < seg_len[i]; k++, tok++) {
+      axis_pos[tok] = s + (W ? k / W / H : k);
+      axis_pos[N + tok] = s + (W ? k / W % H : k);
+      axis_pos[2 * N + tok] = s + (W ? k % W : k);
+    }
+  }
+  return TT_OK;
+}
+
 extern "C" tt_status tt_tree_path_weights(int32_t n_nodes, const int32_t* parent, const int32_t* seg_len,
                                           const uint8_t* trained, int32_t scheme, const float* path_weight,
                                           const float* advantage, float* tok_weight, int32_t* leaf_node) {
