@@ -682,6 +682,95 @@ tt_status tt_tree_gdn_bwd(int64_t n_tokens, int32_t hk, int32_t hv, int32_t dk, 
                           void* workspace, size_t workspace_bytes, void* stream);
 
 /* ------------------------------------------------------------------------------------------
+ * Selective state space scan with tree state routing (device; host helper)
+ *
+ * The recurrent core of a selective state space layer.  Per channel c (of group c / (channels /
+ * groups)) with n_state states, token t with predecessor p on its own root-to-token sequence (h_p =
+ * the initial state at the start of a branch):
+ *     delta = softplus(dt_t[c] + dt_bias[c])            (softplus = 0: dt_t[c] + dt_bias[c] itself)
+ *     h_t[c][n] = exp(delta A[c][n]) h_p[c][n] + delta x_t[c] B_t[n]
+ *     y_t[c] = (sum_n C_t[n] h_t[c][n] + D[c] x_t[c]) silu(z_t[c])   (z = NULL: without the last factor)
+ * i.e. a node's first token continues from the end state of its PARENT node, as in tt_tree_gdn_fwd, and
+ * by the same chunk program: chunk_tok0, chunk_len, chunk_src, chunk_dst, chunk_cap of tt_tree_gdn_plan
+ * (device copies; chunk_cap may be NULL = nothing captured).  The forward takes chunks of any length,
+ * the backward at most TT_GDN_CHUNK tokens (what lies behind them in a longer chunk is not computed).
+ * tt_tree_scan_join (host): the program with the chunks of one run joined as far as the forward is the
+ *   faster for it with this many channels: arrays of n_chunks entries, *n_joined of them written (cap may
+ *   be NULL).  The results are those of the program itself up to rounding.
+ *   x, dt, z, y, dy [n_tokens][channels], b, c [n_tokens][groups][n_state], dtype bf16 or fp32, token
+ *   strides in elements (0 = contiguous); A [channels][n_state] (rates, negative), D, dt_bias [channels]
+ *   or NULL (= 0), fp32; n_state 4, 8 or 16; groups divides channels, and with several groups
+ *   channels / groups is a multiple of 64.  States fp32: initial_state [channels][n_state] or NULL (= 0),
+ *   state_out [n_capture][channels][n_state], given exactly when chunk_cap is.
+ *   All arithmetic is fp32; y is rounded once.
+ * tt_tree_scan_bwd: vector-Jacobian product for dy (stride y_stride_tok); the states are worked out again,
+ *   no forward call is needed.  Outputs, contiguous and overwritten: dx, ddt, dz (like x; dz exactly when z
+ *   is given), dA (like A), db, dc (like b), dD, ddt_bias [channels] fp32 or NULL, d_initial_state
+ *   [channels][n_state] or NULL.  d_state_out: upstream gradient of the captured states, NULL = 0; needs
+ *   chunk_cap.  Gradients that several tokens, channels or branches share are summed in fp32 in a fixed
+ *   order and rounded once.
+ * Outputs may not share memory with inputs.
+ * Alignment: x, dt, z, y, dy and their gradients to the element size; b, c to four elements, with strides
+ *   of a multiple of four; fp32 arrays and the workspace to 16 bytes.
+ * Errors: TT_ERR_NULL, TT_ERR_SHAPE, TT_ERR_DTYPE, TT_ERR_ALIGN, TT_ERR_UNSUPPORTED (n_state, groups),
+ *   TT_ERR_WORKSPACE; the workspace functions return 0 for an invalid descriptor.
+ * ------------------------------------------------------------------------------------------ */
+#define TT_SCAN_CHUNK_MAX 1024      /* most tokens of a joined chunk                                       */
+#define TT_SCAN_MIN_WAVES 12288     /* chunks times blocks of 64 channels below which none are joined further */
+typedef struct {
+  int64_t n_tokens;
+  int32_t channels, n_state, groups;
+  int32_t dtype;                    /* TT_DTYPE_*: type of x, dt, z, b, c, y and their gradients */
+  int32_t softplus;                 /* 1: delta = softplus(dt + dt_bias), 0: dt + dt_bias        */
+  int64_t x_stride_tok, dt_stride_tok, z_stride_tok, b_stride_tok, c_stride_tok, y_stride_tok;
+} tt_scan_desc;
+typedef struct {
+  int32_t n_chunks, n_slots;
+  const int32_t *chunk_tok0, *chunk_len, *chunk_src, *chunk_dst, *chunk_cap;      /* device */
+} tt_scan_chunks;
+tt_status tt_tree_scan_join(int32_t n_chunks, const int32_t* chunk_tok0, const int32_t* chunk_len,
+                            const int32_t* chunk_src, const int32_t* chunk_dst, const int32_t* chunk_cap,
+                            int32_t channels, int32_t* n_joined, int32_t* tok0, int32_t* len, int32_t* src,
+                            int32_t* dst, int32_t* cap);
+size_t tt_tree_scan_fwd_workspace(const tt_scan_desc* desc, int32_t n_chunks, int32_t n_slots);
+size_t tt_tree_scan_bwd_workspace(const tt_scan_desc* desc, int32_t n_chunks, int32_t n_slots);
+tt_status tt_tree_scan_fwd(const tt_scan_desc* desc, const tt_scan_chunks* chunks, const void* x, const void* dt,
+                           const float* A, const void* b, const void* c, const float* D, const void* z,
+                           const float* dt_bias, const float* initial_state, float* state_out, void* y,
+                           void* workspace, size_t workspace_bytes, void* stream);
+tt_status tt_tree_scan_bwd(const tt_scan_desc* desc, const tt_scan_chunks* chunks, const void* x, const void* dt,
+                           const float* A, const void* b, const void* c, const float* D, const void* z,
+                           const float* dt_bias, const float* initial_state, const void* dy,
+                           const float* d_state_out, void* dx, void* ddt, float* dA, void* db, void* dc, float* dD,
+                           void* dz, float* ddt_bias, float* d_initial_state, void* workspace,
+                           size_t workspace_bytes, void* stream);
+
+/* ------------------------------------------------------------------------------------------
+ * One token per row from saved states (device)
+ *
+ * The single-token forms of tt_tree_scan_fwd and tt_tree_conv_fwd: a rollout goes on from the end of a tree
+ * node (state_out of the scan; the node's last K - 1 inputs of the convolution) or from its own last token.
+ * Row r goes on from saved state index[r]; several rows may go on from the same one.  An index outside
+ * [0, n_slots) stands for the start of a sequence (zero state; the indices live in device memory and are not
+ * validated on the host).  index = NULL: row r goes on from state r, n_slots >= n_rows.
+ * tt_tree_scan_step: desc->n_tokens rows of x, dt, z, b, c, y as for tt_tree_scan_fwd; state
+ *   [n_slots][channels][n_state], state_out [n_tokens][channels][n_state], fp32.
+ * tt_tree_conv_step: x, y [n_rows][channels] (row strides in elements, 0 = channels), weight, bias, activation
+ *   as for tt_tree_conv_fwd; state [n_slots][K-1][channels], state_out [n_rows][K-1][channels] in the dtype of
+ *   x: the inputs before the token, the oldest first.  channels a multiple of 4.
+ * state_out may be state itself when index is NULL (in place); otherwise outputs may not share memory with
+ * inputs.
+ * Alignment: as for the scan; the convolution's pointers and rows to four elements, fp32 arrays to 4 bytes.
+ * ------------------------------------------------------------------------------------------ */
+tt_status tt_tree_scan_step(const tt_scan_desc* desc, const void* x, const void* dt, const float* A, const void* b,
+                            const void* c, const float* D, const void* z, const float* dt_bias, int32_t n_slots,
+                            const float* state, const int32_t* index, float* state_out, void* y, void* stream);
+tt_status tt_tree_conv_step(int64_t n_rows, int32_t channels, int32_t kernel_size, int32_t dtype, int32_t activation,
+                            const void* x, int64_t x_stride_row, const float* weight, const float* bias,
+                            int32_t n_slots, const void* state, const int32_t* index, void* state_out, void* y,
+                            int64_t y_stride_row, void* stream);
+
+/* ------------------------------------------------------------------------------------------
  * Per-kernel timing (measurement aid; off by default).  When enabled, every kernel the library
  * launches is bracketed by HIP events on the launch stream.  tt_kernel_timing_read blocks until
  * the recorded events have completed and returns the totals since the last enable.
@@ -712,7 +801,14 @@ tt_status tt_tree_gdn_bwd(int64_t n_tokens, int32_t hk, int32_t hv, int32_t dk, 
 #define TT_KERNEL_ENTROPY_ROWS   23  /* log-prob, entropy and alternatives, one pass over the logits */
 #define TT_KERNEL_ENTROPY_JOIN   24  /* parts of rows joined                                         */
 #define TT_KERNEL_ENTROPY_BWD    25  /* their gradient                                               */
-#define TT_N_KERNELS          26
+#define TT_KERNEL_SCAN_CARRY     26  /* selective scan: chunks from zero (forward; backward: both ends) */
+#define TT_KERNEL_SCAN_STATES    27  /* selective scan: states down (backward: and up) the tree      */
+#define TT_KERNEL_SCAN_OUT       28  /* selective scan: outputs                                      */
+#define TT_KERNEL_SCAN_GRADS     29  /* selective scan backward: per-token gradients                 */
+#define TT_KERNEL_SCAN_SUMS      30  /* selective scan backward: sums over channels and chunks       */
+#define TT_KERNEL_SCAN_STEP      31  /* selective scan, one token per row                            */
+#define TT_KERNEL_CONV_STEP      32  /* causal convolution, one token per row                        */
+#define TT_N_KERNELS          33
 typedef struct {
   double  ms[TT_N_KERNELS];        /* summed kernel time in milliseconds */
   int64_t launches[TT_N_KERNELS];

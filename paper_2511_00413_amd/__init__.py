@@ -9,4 +9,5 @@ from .binding import (  # noqa: F401
     tree_partition_sizes, tree_partition_plan,
     tree_attn_partitioned_workspace, tree_attn_partitioned_fwd, tree_attn_partitioned_bwd,
     tree_rope_axes, tree_axis_positions, LOGPROB_TOP_MAX, tree_logprob_entropy, tree_logprob_entropy_workspace, tree_logprob_entropy_bwd,
+    ScanGrads, tree_scan_workspace, tree_scan_fwd, tree_scan_bwd, tree_scan_step, tree_conv_step,
 )

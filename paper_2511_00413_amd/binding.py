@@ -5,7 +5,7 @@ import contextlib
 import ctypes
 import os
 from dataclasses import dataclass
-from typing import Optional
+from typing import NamedTuple, Optional
 
 import numpy as np
 
@@ -151,6 +151,21 @@ def _lib() -> ctypes.CDLL:
         lib.tt_tree_gdn_bwd.argtypes = [ctypes.c_int64, ctypes.c_int32, ctypes.c_int32, ctypes.c_int32, ctypes.c_int32, ctypes.c_float,
                                         _vp, _vp, _vp, _vp, _vp, _vp, ctypes.c_int32, _vp, _vp, _vp, _vp, ctypes.c_int32, _vp, _vp, _vp, _vp,
                                         _vp, _vp, _vp, _vp, _vp, _vp, _vp, ctypes.c_size_t, _vp]
+        desc, chunks = ctypes.POINTER(_ScanDesc), ctypes.POINTER(_ScanChunks)
+        lib.tt_tree_scan_join.restype = ctypes.c_int32
+        lib.tt_tree_scan_join.argtypes = [ctypes.c_int32] + [_vp] * 5 + [ctypes.c_int32, _c_i32p] + [_vp] * 5
+        for name in ("tt_tree_scan_fwd_workspace", "tt_tree_scan_bwd_workspace"):
+            getattr(lib, name).restype = ctypes.c_size_t
+            getattr(lib, name).argtypes = [desc, ctypes.c_int32, ctypes.c_int32]
+        lib.tt_tree_scan_fwd.restype = ctypes.c_int32
+        lib.tt_tree_scan_fwd.argtypes = [desc, chunks] + [_vp] * 12 + [ctypes.c_size_t, _vp]
+        lib.tt_tree_scan_bwd.restype = ctypes.c_int32
+        lib.tt_tree_scan_bwd.argtypes = [desc, chunks] + [_vp] * 21 + [ctypes.c_size_t, _vp]
+        lib.tt_tree_scan_step.restype = ctypes.c_int32
+        lib.tt_tree_scan_step.argtypes = [desc] + [_vp] * 8 + [ctypes.c_int32] + [_vp] * 5
+        lib.tt_tree_conv_step.restype = ctypes.c_int32
+        lib.tt_tree_conv_step.argtypes = [ctypes.c_int64, ctypes.c_int32, ctypes.c_int32, ctypes.c_int32, ctypes.c_int32, _vp, ctypes.c_int64,
+                                          _vp, _vp, ctypes.c_int32, _vp, _vp, _vp, _vp, ctypes.c_int64, _vp]
         lib.tt_tree_path_weights.restype = ctypes.c_int32
         lib.tt_tree_path_weights.argtypes = [ctypes.c_int32, _vp, _vp, _vp, ctypes.c_int32, _vp, _vp, _vp, _vp]
         lib.tt_tree_partition_sizes.restype = ctypes.c_int32
@@ -173,7 +188,8 @@ def _lib() -> ctypes.CDLL:
 
 KERNEL_NAMES = ("attn_fwd", "loss_fused", "attn_dkdv", "attn_dq", "loss_rows", "loss_sum", "ref_fwd", "ref_bwd",
                 "attn_plan", "attn_reduce", "loss_bwd", "rope", "part_gather", "part_scatter", "conv_fwd", "conv_bwd", "conv_fix", "gdn_prepare", "gdn_scan",
-                "gdn_bwd_fscan", "gdn_bwd_rscan", "gdn_bwd_finish", "rope_axes", "entropy_rows", "entropy_join", "entropy_bwd")
+                "gdn_bwd_fscan", "gdn_bwd_rscan", "gdn_bwd_finish", "rope_axes", "entropy_rows", "entropy_join", "entropy_bwd",
+                "scan_carry", "scan_states", "scan_out", "scan_grads", "scan_sums", "scan_step", "conv_step")
 
 
 class _KernelTimes(ctypes.Structure):
@@ -295,6 +311,17 @@ class ConvPlan:
 GDN_CHUNK = 64
 
 
+class _ScanDesc(ctypes.Structure):
+    _fields_ = [("n_tokens", ctypes.c_int64), ("channels", ctypes.c_int32), ("n_state", ctypes.c_int32), ("groups", ctypes.c_int32),
+                ("dtype", ctypes.c_int32), ("softplus", ctypes.c_int32)] + \
+               [(f"{name}_stride_tok", ctypes.c_int64) for name in ("x", "dt", "z", "b", "c", "y")]
+
+
+class _ScanChunks(ctypes.Structure):
+    _fields_ = [("n_chunks", ctypes.c_int32), ("n_slots", ctypes.c_int32)] + \
+               [(name, _vp) for name in ("chunk_tok0", "chunk_len", "chunk_src", "chunk_dst", "chunk_cap")]
+
+
 class _GdnSchedule(ctypes.Structure):
     _fields_ = [("n_segments", ctypes.c_int32), ("n_levels", ctypes.c_int32), ("level_off", ctypes.c_void_p),
                 ("seg_chunk0", ctypes.c_void_p), ("seg_chunk1", ctypes.c_void_p), ("slot_cons_off", ctypes.c_void_p),
@@ -325,6 +352,7 @@ class GdnPlan:
     slot_cons_off: Optional[np.ndarray] = None
     slot_cons: Optional[np.ndarray] = None
     parallel: bool = True          # False: the device calls walk all chunks in sequence order (for cross-checks)
+    scan_joined: Optional[dict] = None     # (channels, device) -> tt_tree_scan_join's program on that device
 
     @property
     def n_segments(self) -> int:
@@ -341,6 +369,27 @@ class GdnPlan:
             names += ["seg_chunk0", "seg_chunk1", "slot_cons_off", "slot_cons"]
         self.device = {n: torch.from_numpy(getattr(self, n)).to(device) for n in names}
         return self
+
+    def _scan_chunks(self, channels: Optional[int], device, captured: bool):
+        """ctypes tt_scan_chunks on `device`: the program joined for the scan's forward with this many channels, or (None) as
+        it is.  Laid out once per number of channels."""
+        if self.scan_joined is None:
+            self.scan_joined = {}
+        prog = self.scan_joined.get((channels, device))
+        if prog is None:
+            torch = _torch()
+            arrays = [self.chunk_tok0, self.chunk_len, self.chunk_src, self.chunk_dst, self.chunk_cap]
+            if channels is not None:
+                n = ctypes.c_int32(0)
+                out = [np.zeros(self.n_chunks, np.int32) for _ in range(5)]
+                _check(_lib().tt_tree_scan_join(self.n_chunks, *(_hp(a) for a in arrays), channels, ctypes.byref(n), *(_hp(a) for a in out)))
+                arrays = [a[:n.value] for a in out]
+            packed = torch.from_numpy(np.stack(arrays)).to(device)
+            rows = [packed[i].data_ptr() for i in range(5)]
+            n = packed.shape[1]
+            prog = self.scan_joined[(channels, device)] = (packed, _ScanChunks(n, self.n_slots, *rows[:4], None),
+                                                           _ScanChunks(n, self.n_slots, *rows))
+        return prog[2 if captured else 1]
 
     def _schedule(self):
         """ctypes tt_gdn_schedule for the device calls, or None (sequential walk)."""
@@ -1062,3 +1111,168 @@ def tree_gdn_bwd(q, k, v, g, beta, d_o, plan: GdnPlan, *, scale=None, initial_st
                                   _dp(dbeta), _dp(d_init), _dp(workspace), workspace.numel(), _stream_ptr(stream)))
     out = (dq, dk_, dv_, dg, dbeta)
     return out + (d_init,) if want_d_initial_state else out
+
+
+# ---- selective state space scan ----------------------------------------------------------------
+
+class ScanGrads(NamedTuple):
+    """Gradients of tree_scan_fwd's inputs; None where the input was not given (or d_initial_state was not asked for)."""
+    dx: object
+    ddt: object
+    dA: object
+    dB: object
+    dC: object
+    dD: object
+    dz: object
+    ddt_bias: object
+    d_initial_state: object
+
+
+def _scan_desc(x, dt, A, B, C, D, z, dt_bias, softplus) -> _ScanDesc:
+    """Checks what the scan and its single-token form share; the stride of y / dy is filled in by the caller."""
+    torch = _torch()
+    if x.dim() != 2 or A.dim() != 2 or B.dim() != 3:
+        raise ValueError("x must be [tokens, channels], A [channels, states], B and C [tokens, groups, states]")
+    n, ch = x.shape
+    m, groups = A.shape[1], B.shape[1]
+    dtype = x.dtype
+    xs = _check_rows(x, "x", (n, ch), (torch.bfloat16, torch.float32))
+    ds = _check_rows(dt, "dt", (n, ch), (dtype,))
+    bs, cs = _check_rows(B, "B", (n, groups, m), (dtype,)), _check_rows(C, "C", (n, groups, m), (dtype,))
+    zs = _check_rows(z, "z", (n, ch), (dtype,)) if z is not None else 0
+    _check_tensor(A, "A", (ch, m), torch.float32)
+    for name, t in (("D", D), ("dt_bias", dt_bias)):
+        if t is not None:
+            _check_tensor(t, name, (ch,), torch.float32)
+    return _ScanDesc(n, ch, m, groups, DTYPE_BF16 if dtype == torch.bfloat16 else DTYPE_FP32, 1 if softplus else 0, xs, ds, zs, bs, cs, 0)
+
+
+def _check_scan_plan(plan: GdnPlan, n: int) -> None:
+    have = int(plan.chunk_tok0[-1]) + int(plan.chunk_len[-1]) if plan.n_chunks else 0
+    if have != n:
+        raise ValueError(f"the plan is of a tree of {have} tokens, the tensors have {n}")
+
+
+def tree_scan_fwd(x, dt, A, B, C, plan: GdnPlan, *, D=None, z=None, dt_bias=None, softplus: bool = True, initial_state=None,
+                  return_states: bool = False, out=None, workspace=None, stream=None):
+    """Selective state space scan with tree state routing: x, dt [n, channels], B, C [n, groups, states] bf16 or fp32 (free token
+    strides), A [channels, states] fp32 (negative), D, dt_bias [channels] fp32 or None, z [n, channels] (the gate) or None; the
+    chunk program is tree_gdn_plan's.  Returns y [n, channels]; with return_states also the end states [n_capture, channels,
+    states] fp32 of the plan's capture nodes.  initial_state [channels, states] fp32: the state every root starts from."""
+    torch = _torch()
+    desc = _scan_desc(x, dt, A, B, C, D, z, dt_bias, softplus)
+    n, ch, m = desc.n_tokens, desc.channels, desc.n_state
+    _check_scan_plan(plan, n)
+    if initial_state is not None:
+        _check_tensor(initial_state, "initial_state", (ch, m), torch.float32)
+    desc.y_stride_tok = _check_rows(out, "out", (n, ch), (x.dtype,)) if out is not None else ch
+    with _launch_on(x, dt, A, B, C, D, z, dt_bias, initial_state, out, workspace):
+        dev = x.device
+        captured = return_states and plan.n_capture > 0
+        chunks = plan._scan_chunks(ch, dev, captured)
+        if out is None:
+            out = torch.empty((n, ch), dtype=x.dtype, device=dev)
+        states = torch.empty((plan.n_capture, ch, m), dtype=torch.float32, device=dev) if return_states else None
+        need = int(_lib().tt_tree_scan_fwd_workspace(ctypes.byref(desc), chunks.n_chunks, chunks.n_slots))
+        if workspace is None:
+            workspace = torch.empty(max(need, 256), dtype=torch.uint8, device=dev)
+        _check(_lib().tt_tree_scan_fwd(ctypes.byref(desc), ctypes.byref(chunks), _dp(x), _dp(dt), _dp(A), _dp(B), _dp(C), _dp(D), _dp(z),
+                                       _dp(dt_bias), _dp(initial_state), _dp(states) if captured else None, _dp(out), _dp(workspace),
+                                       workspace.numel() * workspace.element_size(), _stream_ptr(stream)))
+    return (out, states) if return_states else out
+
+
+def tree_scan_workspace(x, A, B, plan: GdnPlan, backward: bool = False) -> int:
+    """Bytes of workspace of tree_scan_fwd or tree_scan_bwd for tensors of these shapes."""
+    torch = _torch()
+    desc = _ScanDesc(x.shape[0], x.shape[1], A.shape[1], B.shape[1], DTYPE_BF16 if x.dtype == torch.bfloat16 else DTYPE_FP32, 1)
+    if backward:
+        return int(_lib().tt_tree_scan_bwd_workspace(ctypes.byref(desc), plan.n_chunks, plan.n_slots))
+    return int(_lib().tt_tree_scan_fwd_workspace(ctypes.byref(desc), plan.n_chunks, plan.n_slots))
+
+
+def tree_scan_bwd(x, dt, A, B, C, d_y, plan: GdnPlan, *, D=None, z=None, dt_bias=None, softplus: bool = True, initial_state=None,
+                  d_state_out=None, want_d_initial_state: bool = False, workspace=None, stream=None) -> ScanGrads:
+    """Backward of tree_scan_fwd for upstream d_y [n, channels] (dtype of x, free token stride).  d_state_out [n_capture, channels,
+    states] fp32: upstream gradient of the plan's captured end states.  Returns ScanGrads: dx, ddt, dz like x, dB, dC like B, dA,
+    dD, ddt_bias, d_initial_state fp32."""
+    torch = _torch()
+    desc = _scan_desc(x, dt, A, B, C, D, z, dt_bias, softplus)
+    n, ch, m, groups = desc.n_tokens, desc.channels, desc.n_state, desc.groups
+    _check_scan_plan(plan, n)
+    if initial_state is not None:
+        _check_tensor(initial_state, "initial_state", (ch, m), torch.float32)
+    if d_state_out is not None:
+        _check_tensor(d_state_out, "d_state_out", (plan.n_capture, ch, m), torch.float32)
+    desc.y_stride_tok = _check_rows(d_y, "d_y", (n, ch), (x.dtype,))
+    with _launch_on(x, dt, A, B, C, D, z, dt_bias, initial_state, d_y, d_state_out, workspace):
+        dev = x.device
+        captured = d_state_out is not None and plan.n_capture > 0
+        chunks = plan._scan_chunks(None, dev, captured)
+        like = lambda t: None if t is None else torch.empty(t.shape, dtype=t.dtype, device=dev)      # noqa: E731
+        grads = ScanGrads(like(x), like(x), like(A), like(B), like(C), like(D), like(z), like(dt_bias), like(A) if want_d_initial_state else None)
+        need = int(_lib().tt_tree_scan_bwd_workspace(ctypes.byref(desc), chunks.n_chunks, chunks.n_slots))
+        if workspace is None:
+            workspace = torch.empty(max(need, 256), dtype=torch.uint8, device=dev)
+        _check(_lib().tt_tree_scan_bwd(ctypes.byref(desc), ctypes.byref(chunks), _dp(x), _dp(dt), _dp(A), _dp(B), _dp(C), _dp(D), _dp(z),
+                                       _dp(dt_bias), _dp(initial_state), _dp(d_y), _dp(d_state_out) if captured else None,
+                                       *(_dp(g) for g in grads), _dp(workspace), workspace.numel() * workspace.element_size(),
+                                       _stream_ptr(stream)))
+    return grads
+
+
+def tree_scan_step(x, dt, A, B, C, state, *, index=None, D=None, z=None, dt_bias=None, softplus: bool = True, state_out=None, out=None,
+                   stream=None):
+    """One token per row: tree_scan_fwd's recurrence from saved states.  x, dt, z [rows, channels], B, C [rows, groups, states]; state
+    [slots, channels, states] fp32.  Row r goes on from state index[r] (int32; several rows may share one, an index outside the
+    states starts from zero) or, without an index, from state r.  Returns (y [rows, channels], state_out [rows, channels, states]);
+    state_out may be state itself (in place) when there is no index."""
+    torch = _torch()
+    desc = _scan_desc(x, dt, A, B, C, D, z, dt_bias, softplus)
+    n, ch, m = desc.n_tokens, desc.channels, desc.n_state
+    slots = state.shape[0]
+    _check_tensor(state, "state", (slots, ch, m), torch.float32)
+    if index is not None:
+        _check_tensor(index, "index", (n,), torch.int32)
+    if state_out is not None:
+        _check_tensor(state_out, "state_out", (slots if state_out is state else n, ch, m), torch.float32)
+    desc.y_stride_tok = _check_rows(out, "out", (n, ch), (x.dtype,)) if out is not None else ch
+    with _launch_on(x, dt, A, B, C, D, z, dt_bias, state, index, state_out, out):
+        if out is None:
+            out = torch.empty((n, ch), dtype=x.dtype, device=x.device)
+        if state_out is None:
+            state_out = torch.empty((n, ch, m), dtype=torch.float32, device=x.device)
+        _check(_lib().tt_tree_scan_step(ctypes.byref(desc), _dp(x), _dp(dt), _dp(A), _dp(B), _dp(C), _dp(D), _dp(z), _dp(dt_bias), slots,
+                                        _dp(state), _dp(index), _dp(state_out), _dp(out), _stream_ptr(stream)))
+    return out, state_out
+
+
+def tree_conv_step(x, state, weight, bias=None, *, index=None, silu: bool = True, state_out=None, out=None, stream=None):
+    """One token per row: tree_conv_fwd from saved contexts.  x [rows, C] bf16/fp32 (free row stride), state [slots, K-1, C] like x:
+    the inputs before the token, the oldest first; weight [C, K], bias [C] fp32.  index and state_out as in tree_scan_step.
+    Returns (y [rows, C], state_out [rows, K-1, C])."""
+    torch = _torch()
+    if x.dim() != 2 or weight.dim() != 2:
+        raise ValueError("x must be [rows, channels], weight [channels, taps]")
+    n, c = x.shape
+    k = weight.shape[1]
+    xs = _check_rows(x, "x", (n, c), (torch.bfloat16, torch.float32))
+    slots = state.shape[0]
+    _check_tensor(state, "state", (slots, k - 1, c), x.dtype)
+    _check_tensor(weight, "weight", (c, k), torch.float32)
+    if bias is not None:
+        _check_tensor(bias, "bias", (c,), torch.float32)
+    if index is not None:
+        _check_tensor(index, "index", (n,), torch.int32)
+    if state_out is not None:
+        _check_tensor(state_out, "state_out", (slots if state_out is state else n, k - 1, c), x.dtype)
+    ys = _check_rows(out, "out", (n, c), (x.dtype,)) if out is not None else c
+    with _launch_on(x, state, weight, bias, index, state_out, out):
+        if out is None:
+            out = torch.empty((n, c), dtype=x.dtype, device=x.device)
+        if state_out is None:
+            state_out = torch.empty((n, k - 1, c), dtype=x.dtype, device=x.device)
+        _check(_lib().tt_tree_conv_step(n, c, k, DTYPE_BF16 if x.dtype == torch.bfloat16 else DTYPE_FP32, 1 if silu else 0, _dp(x), xs,
+                                        _dp(weight), _dp(bias), slots, _dp(state), _dp(index), _dp(state_out), _dp(out), ys,
+                                        _stream_ptr(stream)))
+    return out, state_out

@@ -1,6 +1,7 @@
 // C ABI entry points of the device calls: argument validation on the host, then dispatch to the
 // kernels.  Nothing is launched unless every check passes.
 #include <hip/hip_runtime.h>
+#include <algorithm>
 #include <climits>
 #include <cmath>
 #include <mutex>
@@ -621,4 +622,237 @@ extern "C" tt_status tt_tree_gdn_bwd(int64_t n_tokens, int32_t hk, int32_t hv, i
   a.dq = dq; a.dk = dk_out; a.dv = dv_out; a.dg = dg; a.dbeta = dbeta; a.d_initial_state = d_initial_state;
   a.workspace = workspace; a.workspace_bytes = workspace_bytes;
   return hip_result(tt::gdn_bwd(a, (hipStream_t)stream), "tree_gdn_bwd");
+}
+
+namespace {
+
+struct Span { const void* p; int64_t bytes; };
+bool meets(const Span& a, const Span& b) {
+  const uintptr_t a0 = reinterpret_cast<uintptr_t>(a.p), b0 = reinterpret_cast<uintptr_t>(b.p);
+  return a.p && b.p && a.bytes > 0 && b.bytes > 0 && a0 < b0 + (uintptr_t)b.bytes && b0 < a0 + (uintptr_t)a.bytes;
+}
+
+// Rows of `len` elements, `step` apart.
+struct Rows {
+  const void* p;
+  int64_t n, len, step, es;
+  Span span() const { return {p, n > 0 ? ((n - 1) * step + len) * es : 0}; }
+};
+// Whether an output lies on an input: exact for rows of equal step (slices of one buffer), by their extents otherwise.
+bool meets(const Rows& a, const Rows& b) {
+  if (!a.p || !b.p || a.n <= 0 || b.n <= 0) return false;
+  if (a.step == b.step && a.n == b.n) return shares_memory(a.p, a.step * a.es, b.p, b.step * b.es, std::max(a.len, b.len) * a.es, a.n);
+  return meets(a.span(), b.span());
+}
+
+bool aligned_to(const void* p, size_t n) { return reinterpret_cast<uintptr_t>(p) % n == 0; }
+
+// Sizes and strides of a scan descriptor; strides of 0 are filled in.
+tt_status check_scan_desc(const tt_scan_desc* in, tt_scan_desc& d) {
+  if (!in) return fail(TT_ERR_NULL, "desc is NULL");
+  d = *in;
+  if (d.dtype != TT_DTYPE_BF16 && d.dtype != TT_DTYPE_FP32) return fail(TT_ERR_DTYPE, "unknown dtype %d", d.dtype);
+  if (d.n_tokens < 0 || d.n_tokens >= INT32_MAX) return fail(TT_ERR_SHAPE, "n_tokens=%lld out of range", (long long)d.n_tokens);
+  if (d.channels <= 0 || d.channels > (1 << 20)) return fail(TT_ERR_SHAPE, "channels=%d must lie in [1, %d]", d.channels, 1 << 20);
+  if (d.n_state != 4 && d.n_state != 8 && d.n_state != 16) return fail(TT_ERR_UNSUPPORTED, "n_state=%d: 4, 8 and 16 are built", d.n_state);
+  if (d.groups <= 0 || d.channels % d.groups) return fail(TT_ERR_SHAPE, "groups=%d must divide channels=%d", d.groups, d.channels);
+  if (d.groups > 1 && d.channels / d.groups % 64)
+    return fail(TT_ERR_UNSUPPORTED, "with several groups a group must be a multiple of 64 channels, not %d", d.channels / d.groups);
+  if (d.softplus != 0 && d.softplus != 1) return fail(TT_ERR_UNSUPPORTED, "softplus=%d: 0 or 1", d.softplus);
+  const int64_t c = d.channels, bc = (int64_t)d.groups * d.n_state;
+  for (int64_t* s : {&d.x_stride_tok, &d.dt_stride_tok, &d.z_stride_tok, &d.y_stride_tok}) {
+    if (*s == 0) *s = c;
+    if (*s < c) return fail(TT_ERR_SHAPE, "token stride %lld is smaller than channels=%lld", (long long)*s, (long long)c);
+  }
+  for (int64_t* s : {&d.b_stride_tok, &d.c_stride_tok}) {
+    if (*s == 0) *s = bc;
+    if (*s < bc) return fail(TT_ERR_SHAPE, "token stride %lld is smaller than groups * n_state=%lld", (long long)*s, (long long)bc);
+    if (*s % 4) return fail(TT_ERR_ALIGN, "token strides of b and c must be multiples of 4 elements, not %lld", (long long)*s);
+  }
+  return TT_OK;
+}
+
+// Inputs that the scan and its single-token form share.
+tt_status check_scan_inputs(const tt_scan_desc& d, const void* x, const void* dt, const float* A, const void* b, const void* c,
+                            const float* D, const void* z, const float* dt_bias) {
+  if (!A) return fail(TT_ERR_NULL, "A is NULL");
+  if (d.n_tokens > 0 && (!x || !dt || !b || !c)) return fail(TT_ERR_NULL, "x / dt / b / c is NULL");
+  const size_t es = d.dtype == TT_DTYPE_BF16 ? 2 : 4;
+  for (const void* p : {x, dt, z})
+    if (!aligned_to(p, es)) return fail(TT_ERR_ALIGN, "x / dt / z is not aligned to its element size");
+  for (const void* p : {b, c})
+    if (!aligned_to(p, 4 * es)) return fail(TT_ERR_ALIGN, "b / c is not aligned to four elements");
+  for (const float* p : {A, D, dt_bias})
+    if (!tt::aligned16(p)) return fail(TT_ERR_ALIGN, "A / D / dt_bias is not 16-byte aligned");
+  return TT_OK;
+}
+
+tt_status check_scan_chunks(const tt_scan_desc& d, const tt_scan_chunks* k) {
+  if (!k) return fail(TT_ERR_NULL, "chunks is NULL");
+  if (k->n_chunks < 0 || k->n_slots < 0) return fail(TT_ERR_SHAPE, "n_chunks=%d, n_slots=%d", k->n_chunks, k->n_slots);
+  if ((d.n_tokens > 0) != (k->n_chunks > 0) || k->n_chunks > d.n_tokens || k->n_slots > k->n_chunks)
+    return fail(TT_ERR_SHAPE, "n_tokens=%lld with %d chunks and %d saved states", (long long)d.n_tokens, k->n_chunks, k->n_slots);
+  // a dimension of a launch holds less than 2^32 work-items
+  if (((int64_t)d.channels + 255) / 256 * k->n_chunks >= 1 << 24 || d.n_tokens * d.groups * d.n_state >= (int64_t)1 << 30)
+    return fail(TT_ERR_SHAPE, "%d chunks of %d channels (%d groups of %d states) are more than one launch holds", k->n_chunks, d.channels,
+                d.groups, d.n_state);
+  if (k->n_chunks > 0 && (!k->chunk_tok0 || !k->chunk_len || !k->chunk_src || !k->chunk_dst))
+    return fail(TT_ERR_NULL, "a chunk array is NULL");
+  return TT_OK;
+}
+
+tt::ScanArgs scan_args(const tt_scan_desc& d, const tt_scan_chunks& k) {
+  tt::ScanArgs a{};
+  a.n_tokens = (int)d.n_tokens; a.channels = d.channels; a.n_state = d.n_state; a.groups = d.groups;
+  a.n_chunks = k.n_chunks; a.n_slots = k.n_slots; a.bf16 = d.dtype == TT_DTYPE_BF16; a.use_softplus = d.softplus == 1;
+  a.x_stride = d.x_stride_tok; a.dt_stride = d.dt_stride_tok; a.z_stride = d.z_stride_tok; a.b_stride = d.b_stride_tok;
+  a.c_stride = d.c_stride_tok; a.y_stride = a.dy_stride = d.y_stride_tok;
+  a.chunk_tok0 = k.chunk_tok0; a.chunk_len = k.chunk_len; a.chunk_src = k.chunk_src; a.chunk_dst = k.chunk_dst; a.chunk_cap = k.chunk_cap;
+  return a;
+}
+
+}  // namespace
+
+extern "C" size_t tt_tree_scan_fwd_workspace(const tt_scan_desc* desc, int32_t n_chunks, int32_t n_slots) {
+  tt::clear_error();
+  tt_scan_desc d;
+  if (check_scan_desc(desc, d) || n_chunks < 0 || n_slots < 0) return 0;
+  return tt::scan_fwd_workspace(d.channels, d.n_state, n_chunks, n_slots);
+}
+
+extern "C" size_t tt_tree_scan_bwd_workspace(const tt_scan_desc* desc, int32_t n_chunks, int32_t n_slots) {
+  tt::clear_error();
+  tt_scan_desc d;
+  if (check_scan_desc(desc, d) || n_chunks < 0 || n_slots < 0) return 0;
+  return tt::scan_bwd_workspace(d.n_tokens, d.channels, d.n_state, d.groups, n_chunks, n_slots);
+}
+
+extern "C" tt_status tt_tree_scan_fwd(const tt_scan_desc* desc, const tt_scan_chunks* chunks, const void* x, const void* dt,
+                                      const float* A, const void* b, const void* c, const float* D, const void* z,
+                                      const float* dt_bias, const float* initial_state, float* state_out, void* y, void* workspace,
+                                      size_t workspace_bytes, void* stream) {
+  tt::clear_error();
+  tt_scan_desc d;
+  if (tt_status s = check_scan_desc(desc, d)) return s;
+  if (tt_status s = check_scan_chunks(d, chunks)) return s;
+  if (tt_status s = check_scan_inputs(d, x, dt, A, b, c, D, z, dt_bias)) return s;
+  if (d.n_tokens > 0 && !y) return fail(TT_ERR_NULL, "y is NULL");
+  if ((chunks->chunk_cap != nullptr) != (state_out != nullptr)) return fail(TT_ERR_NULL, "chunk_cap and state_out must be given together");
+  const int64_t es = d.dtype == TT_DTYPE_BF16 ? 2 : 4, n = d.n_tokens, width = (int64_t)d.channels * d.n_state * 4;
+  if (!aligned_to(y, es)) return fail(TT_ERR_ALIGN, "y is not aligned to its element size");
+  if (!tt::aligned16(initial_state) || !tt::aligned16(state_out)) return fail(TT_ERR_ALIGN, "a state is not 16-byte aligned");
+  const int64_t bc = (int64_t)d.groups * d.n_state;
+  const Rows out{y, n, d.channels, d.y_stride_tok, es};
+  for (const Rows& in : {Rows{x, n, d.channels, d.x_stride_tok, es}, Rows{dt, n, d.channels, d.dt_stride_tok, es},
+                         Rows{z, n, d.channels, d.z_stride_tok, es}, Rows{b, n, bc, d.b_stride_tok, es}, Rows{c, n, bc, d.c_stride_tok, es}})
+    if (meets(out, in)) return fail(TT_ERR_SHAPE, "y shares memory with an input");
+  if (meets(Span{state_out, state_out ? width : 0}, Span{initial_state, width})) return fail(TT_ERR_SHAPE, "state_out shares memory with initial_state");
+  const size_t need = tt::scan_fwd_workspace(d.channels, d.n_state, chunks->n_chunks, chunks->n_slots);
+  if (!workspace || workspace_bytes < need || !tt::aligned16(workspace))
+    return fail(TT_ERR_WORKSPACE, "scan forward needs %zu bytes of 16-byte aligned workspace, got %zu", need, workspace_bytes);
+  tt::ScanArgs a = scan_args(d, *chunks);
+  a.x = x; a.dt = dt; a.A = A; a.b = b; a.c = c; a.D = D; a.z = z; a.dt_bias = dt_bias;
+  a.initial_state = initial_state; a.state_out = state_out; a.y = y; a.workspace = workspace;
+  return hip_result(tt::scan_fwd(a, (hipStream_t)stream), "tree_scan_fwd");
+}
+
+extern "C" tt_status tt_tree_scan_bwd(const tt_scan_desc* desc, const tt_scan_chunks* chunks, const void* x, const void* dt,
+                                      const float* A, const void* b, const void* c, const float* D, const void* z,
+                                      const float* dt_bias, const float* initial_state, const void* dy, const float* d_state_out,
+                                      void* dx, void* ddt, float* dA, void* db, void* dc, float* dD, void* dz, float* ddt_bias,
+                                      float* d_initial_state, void* workspace, size_t workspace_bytes, void* stream) {
+  tt::clear_error();
+  tt_scan_desc d;
+  if (tt_status s = check_scan_desc(desc, d)) return s;
+  if (tt_status s = check_scan_chunks(d, chunks)) return s;
+  if (tt_status s = check_scan_inputs(d, x, dt, A, b, c, D, z, dt_bias)) return s;
+  if (!dA || (d.n_tokens > 0 && (!dy || !dx || !ddt || !db || !dc))) return fail(TT_ERR_NULL, "dy / dx / ddt / dA / db / dc is NULL");
+  if (d.n_tokens > 0 && (z != nullptr) != (dz != nullptr)) return fail(TT_ERR_NULL, "dz must be given exactly when z is");
+  if (d_state_out && !chunks->chunk_cap) return fail(TT_ERR_NULL, "d_state_out needs chunk_cap");
+  const int64_t es = d.dtype == TT_DTYPE_BF16 ? 2 : 4, n = d.n_tokens, ch = d.channels, bc = (int64_t)d.groups * d.n_state;
+  for (const void* p : {dy, (const void*)dx, (const void*)ddt, (const void*)db, (const void*)dc, (const void*)dz})
+    if (!aligned_to(p, es)) return fail(TT_ERR_ALIGN, "a tensor is not aligned to its element size");
+  for (const float* p : {initial_state, d_state_out, (const float*)dA, (const float*)dD, (const float*)ddt_bias, (const float*)d_initial_state})
+    if (!tt::aligned16(p)) return fail(TT_ERR_ALIGN, "an fp32 array is not 16-byte aligned");
+  const Rows ins[] = {{x, n, ch, d.x_stride_tok, es}, {dt, n, ch, d.dt_stride_tok, es}, {z, n, ch, d.z_stride_tok, es},
+                      {dy, n, ch, d.y_stride_tok, es}, {b, n, bc, d.b_stride_tok, es}, {c, n, bc, d.c_stride_tok, es},
+                      {A, 1, ch * d.n_state, ch * d.n_state, 4}, {D, 1, ch, ch, 4}, {dt_bias, 1, ch, ch, 4},
+                      {initial_state, 1, ch * d.n_state, ch * d.n_state, 4}, {d_state_out, 1, ch * d.n_state, ch * d.n_state, 4}};
+  const Span outs[] = {{dx, n * ch * es}, {ddt, n * ch * es}, {dz, n * ch * es}, {db, n * bc * es}, {dc, n * bc * es},
+                       {dA, ch * d.n_state * 4}, {dD, ch * 4}, {ddt_bias, ch * 4}, {d_initial_state, ch * d.n_state * 4}};
+  for (const Span& o : outs) {
+    for (const Rows& i : ins)
+      if (meets(o, i.span())) return fail(TT_ERR_SHAPE, "an output shares memory with an input");
+    for (const Span& p : outs)
+      if (&p != &o && meets(o, p)) return fail(TT_ERR_SHAPE, "two outputs share memory");
+  }
+  const size_t need = tt::scan_bwd_workspace(n, d.channels, d.n_state, d.groups, chunks->n_chunks, chunks->n_slots);
+  if (!workspace || workspace_bytes < need || !tt::aligned16(workspace))
+    return fail(TT_ERR_WORKSPACE, "scan backward needs %zu bytes of 16-byte aligned workspace, got %zu", need, workspace_bytes);
+  tt::ScanArgs a = scan_args(d, *chunks);
+  if (!d_state_out) a.chunk_cap = nullptr;
+  a.x = x; a.dt = dt; a.A = A; a.b = b; a.c = c; a.D = D; a.z = z; a.dt_bias = dt_bias; a.initial_state = initial_state;
+  a.dy = dy; a.d_state_out = d_state_out; a.dx = dx; a.ddt = ddt; a.dA = dA; a.db = db; a.dc = dc; a.dD = dD; a.dz = dz;
+  a.ddt_bias = ddt_bias; a.d_initial_state = d_initial_state; a.workspace = workspace;
+  return hip_result(tt::scan_bwd(a, (hipStream_t)stream), "tree_scan_bwd");
+}
+
+extern "C" tt_status tt_tree_scan_step(const tt_scan_desc* desc, const void* x, const void* dt, const float* A, const void* b,
+                                       const void* c, const float* D, const void* z, const float* dt_bias, int32_t n_slots,
+                                       const float* state, const int32_t* index, float* state_out, void* y, void* stream) {
+  tt::clear_error();
+  tt_scan_desc d;
+  if (tt_status s = check_scan_desc(desc, d)) return s;
+  if (tt_status s = check_scan_inputs(d, x, dt, A, b, c, D, z, dt_bias)) return s;
+  const int64_t n = d.n_tokens, es = d.dtype == TT_DTYPE_BF16 ? 2 : 4, width = (int64_t)d.channels * d.n_state, bc = (int64_t)d.groups * d.n_state;
+  if (n_slots < 0 || (!index && n_slots < n)) return fail(TT_ERR_SHAPE, "n_slots=%d for %lld rows", n_slots, (long long)n);
+  if (n > 0 && (!state_out || !y || (n_slots > 0 && !state))) return fail(TT_ERR_NULL, "state / state_out / y is NULL");
+  if (!aligned_to(y, es)) return fail(TT_ERR_ALIGN, "y is not aligned to its element size");
+  if (!tt::aligned16(state) || !tt::aligned16(state_out)) return fail(TT_ERR_ALIGN, "a state is not 16-byte aligned");
+  if (!(state_out == state && !index) && meets(Span{state_out, n * width * 4}, Span{state, n_slots * width * 4}))
+    return fail(TT_ERR_SHAPE, "state_out may share memory with state only as a whole and without an index");
+  const Rows out{y, n, d.channels, d.y_stride_tok, es};
+  for (const Rows& in : {Rows{x, n, d.channels, d.x_stride_tok, es}, Rows{dt, n, d.channels, d.dt_stride_tok, es},
+                         Rows{z, n, d.channels, d.z_stride_tok, es}, Rows{b, n, bc, d.b_stride_tok, es}, Rows{c, n, bc, d.c_stride_tok, es}})
+    if (meets(out, in)) return fail(TT_ERR_SHAPE, "y shares memory with an input");
+  tt::ScanStepArgs a{};
+  a.n_rows = (int)n; a.channels = d.channels; a.n_state = d.n_state; a.groups = d.groups; a.n_slots = n_slots; a.use_softplus = d.softplus == 1;
+  a.x = x; a.dt = dt; a.z = z; a.b = b; a.c = c; a.A = A; a.D = D; a.dt_bias = dt_bias; a.state = state; a.index = index;
+  a.x_stride = d.x_stride_tok; a.dt_stride = d.dt_stride_tok; a.z_stride = d.z_stride_tok; a.b_stride = d.b_stride_tok;
+  a.c_stride = d.c_stride_tok; a.y_stride = d.y_stride_tok; a.state_out = state_out; a.y = y;
+  return hip_result(tt::scan_step(a, d.dtype == TT_DTYPE_BF16, (hipStream_t)stream), "tree_scan_step");
+}
+
+extern "C" tt_status tt_tree_conv_step(int64_t n_rows, int32_t channels, int32_t kernel_size, int32_t dtype, int32_t activation,
+                                       const void* x, int64_t x_stride_row, const float* weight, const float* bias, int32_t n_slots,
+                                       const void* state, const int32_t* index, void* state_out, void* y, int64_t y_stride_row,
+                                       void* stream) {
+  tt::clear_error();
+  if (dtype != TT_DTYPE_BF16 && dtype != TT_DTYPE_FP32) return fail(TT_ERR_DTYPE, "unknown dtype %d", dtype);
+  if (n_rows < 0 || n_rows >= INT32_MAX) return fail(TT_ERR_SHAPE, "n_rows=%lld out of range", (long long)n_rows);
+  if (kernel_size < 2 || kernel_size > 4) return fail(TT_ERR_UNSUPPORTED, "kernel_size=%d: only 2, 3, 4 are built", kernel_size);
+  if (activation != 0 && activation != 1) return fail(TT_ERR_UNSUPPORTED, "activation=%d: 0 (none) or 1 (SiLU)", activation);
+  if (channels <= 0 || channels % 4) return fail(TT_ERR_SHAPE, "channels=%d must be a positive multiple of 4", channels);
+  if (x_stride_row == 0) x_stride_row = channels;
+  if (y_stride_row == 0) y_stride_row = channels;
+  if (x_stride_row < channels || y_stride_row < channels || x_stride_row % 4 || y_stride_row % 4)
+    return fail(TT_ERR_ALIGN, "row strides %lld / %lld must be >= channels and a multiple of 4 elements", (long long)x_stride_row,
+                (long long)y_stride_row);
+  if (!weight) return fail(TT_ERR_NULL, "weight is NULL");
+  if (n_slots < 0 || (!index && n_slots < n_rows)) return fail(TT_ERR_SHAPE, "n_slots=%d for %lld rows", n_slots, (long long)n_rows);
+  if (n_rows > 0 && (!x || !y || !state_out || (n_slots > 0 && !state))) return fail(TT_ERR_NULL, "x / y / state / state_out is NULL");
+  const int64_t es = dtype == TT_DTYPE_BF16 ? 2 : 4, saved = (int64_t)(kernel_size - 1) * channels * es;
+  for (const void* p : {x, (const void*)y, state, (const void*)state_out})
+    if (!aligned_to(p, 4 * es)) return fail(TT_ERR_ALIGN, "a tensor is not aligned to four elements");
+  if (!(state_out == state && !index) && meets(Span{state_out, n_rows * saved}, Span{state, n_slots * saved}))
+    return fail(TT_ERR_SHAPE, "state_out may share memory with state only as a whole and without an index");
+  const Rows in{x, n_rows, channels, x_stride_row, es}, out{y, n_rows, channels, y_stride_row, es};
+  if (meets(out, in) || meets(out.span(), Span{state, n_slots * saved}) || meets(out.span(), Span{state_out, n_rows * saved}) ||
+      meets(in.span(), Span{state_out, n_rows * saved}))
+    return fail(TT_ERR_SHAPE, "an output shares memory with another tensor");
+  tt::ConvStepArgs a{};
+  a.n_rows = (int)n_rows; a.channels = channels; a.n_slots = n_slots; a.silu = activation;
+  a.x = x; a.state = state; a.x_stride = x_stride_row; a.y_stride = y_stride_row; a.weight = weight; a.bias = bias; a.index = index;
+  a.y = y; a.state_out = state_out;
+  return hip_result(tt::conv_step(a, kernel_size, dtype == TT_DTYPE_BF16, (hipStream_t)stream), "tree_conv_step");
 }

@@ -159,4 +159,48 @@ hipError_t gdn_bwd(const GdnBwdArgs& a, hipStream_t st);
 // workspace for passes of key_heads_per_pass key heads (with their hv / hk value heads) at a time
 size_t gdn_bwd_workspace(int64_t n_tokens, int n_chunks, int n_slots, int n_segments, int hk, int hv, int key_heads_per_pass);
 
+// selective state space scan with tree state routing (tt_scan.hip, tt_scan_bwd.hip); strides in elements
+struct ScanArgs {
+  int n_tokens, channels, n_state, groups, n_chunks, n_slots;
+  bool bf16, use_softplus;
+  const void *x, *dt, *z, *b, *c, *dy;            // z: nullptr = no gate; dy: backward only
+  int64_t x_stride, dt_stride, z_stride, b_stride, c_stride, dy_stride;
+  const float *A, *D, *dt_bias;                   // [channels][n_state], [channels] or nullptr
+  const int32_t *chunk_tok0, *chunk_len, *chunk_src, *chunk_dst, *chunk_cap;
+  const float* initial_state;                     // [channels][n_state] or nullptr
+  void* y;                                        // forward
+  int64_t y_stride;
+  float* state_out;                               // [n_capture][channels][n_state]
+  const float* d_state_out;                       // backward; the outputs are contiguous
+  void *dx, *ddt, *db, *dc, *dz;
+  float *dA, *dD, *ddt_bias, *d_initial_state;
+  void* workspace;
+};
+size_t scan_fwd_workspace(int channels, int n_state, int n_chunks, int n_slots);
+hipError_t scan_fwd(const ScanArgs& a, hipStream_t st);
+size_t scan_bwd_workspace(int64_t n_tokens, int channels, int n_state, int groups, int n_chunks, int n_slots);
+hipError_t scan_bwd(const ScanArgs& a, hipStream_t st);
+
+// one token per row from saved states (tt_step.hip); strides in elements
+struct ScanStepArgs {
+  int n_rows, channels, n_state, groups, n_slots;
+  bool use_softplus;
+  const void *x, *dt, *z, *b, *c;
+  int64_t x_stride, dt_stride, z_stride, b_stride, c_stride, y_stride;
+  const float *A, *D, *dt_bias, *state;
+  const int32_t* index;                           // nullptr: row r goes on from state r
+  float* state_out;
+  void* y;
+};
+hipError_t scan_step(const ScanStepArgs& a, bool bf16, hipStream_t st);
+struct ConvStepArgs {
+  int n_rows, channels, n_slots, silu;
+  const void *x, *state;
+  int64_t x_stride, y_stride;
+  const float *weight, *bias;
+  const int32_t* index;
+  void *y, *state_out;
+};
+hipError_t conv_step(const ConvStepArgs& a, int kernel_size, bool bf16, hipStream_t st);
+
 }  // namespace tt

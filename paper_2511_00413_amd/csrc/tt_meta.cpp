@@ -518,3 +518,49 @@ extern "C" tt_status tt_tree_gdn_plan(int32_t n_nodes, const int32_t* parent, co
   }
   return TT_OK;
 }
+
+namespace {
+// One chunk for every maximal run of chunks whose state stays on chip, cut where the run would pass max_tokens.
+template <typename Emit>
+int32_t join_chunks(int32_t n_chunks, const int32_t* len, const int32_t* src, const int32_t* dst, const int32_t* cap, int64_t max_tokens,
+                    Emit emit) {
+  int32_t n = 0;
+  for (int32_t c = 0; c < n_chunks;) {
+    int32_t e = c + 1;
+    int64_t tokens = len[c];
+    while (e < n_chunks && src[e] == -2 && dst[e - 1] < 0 && (!cap || cap[e - 1] < 0) && tokens + len[e] <= max_tokens) tokens += len[e++];
+    emit(n++, c, e, (int32_t)tokens);
+    c = e;
+  }
+  return n;
+}
+}  // namespace
+
+extern "C" tt_status tt_tree_scan_join(int32_t n_chunks, const int32_t* chunk_tok0, const int32_t* chunk_len, const int32_t* chunk_src,
+                                       const int32_t* chunk_dst, const int32_t* chunk_cap, int32_t channels, int32_t* n_joined,
+                                       int32_t* tok0, int32_t* len, int32_t* src, int32_t* dst, int32_t* cap) {
+  tt::clear_error();
+  if (n_chunks < 0 || channels <= 0) return tt::fail(TT_ERR_SHAPE, "n_chunks=%d, channels=%d", n_chunks, channels);
+  if (!n_joined || (n_chunks > 0 && (!chunk_tok0 || !chunk_len || !chunk_src || !chunk_dst || !tok0 || !len || !src || !dst)) ||
+      (cap && !chunk_cap))
+    return tt::fail(TT_ERR_NULL, "an array is NULL");
+  for (int32_t c = 0; c < n_chunks; c++) {
+    if (chunk_len[c] <= 0 || chunk_tok0[c] < 0 || (int64_t)chunk_tok0[c] + chunk_len[c] > INT32_MAX)
+      return tt::fail(TT_ERR_TREE, "chunk %d: %d tokens from %d", c, chunk_len[c], chunk_tok0[c]);
+    if (chunk_src[c] == -2 && (c == 0 || chunk_tok0[c] != chunk_tok0[c - 1] + chunk_len[c - 1]))
+      return tt::fail(TT_ERR_TREE, "chunk %d continues no chunk", c);
+  }
+  // Longer chunks leave fewer end states to be worked out before the outputs can be (the last chunk of a branch needs none) and
+  // fewer states to store; shorter ones spread over more waves.  Doubled as long as enough waves are left to even out.
+  const int64_t waves = ((int64_t)channels + 63) / 64;
+  auto none = [](int32_t, int32_t, int32_t, int32_t) {};
+  int64_t max_tokens = TT_GDN_CHUNK;
+  while (max_tokens < TT_SCAN_CHUNK_MAX &&
+         waves * join_chunks(n_chunks, chunk_len, chunk_src, chunk_dst, chunk_cap, 2 * max_tokens, none) >= TT_SCAN_MIN_WAVES)
+    max_tokens *= 2;
+  *n_joined = join_chunks(n_chunks, chunk_len, chunk_src, chunk_dst, chunk_cap, max_tokens, [&](int32_t i, int32_t c, int32_t e, int32_t n) {
+    tok0[i] = chunk_tok0[c]; len[i] = n; src[i] = chunk_src[c]; dst[i] = chunk_dst[e - 1];
+    if (cap) cap[i] = chunk_cap[e - 1];
+  });
+  return TT_OK;
+}
