@@ -692,13 +692,14 @@ tt_status tt_tree_gdn_bwd(int64_t n_tokens, int32_t hk, int32_t hv, int32_t dk, 
  *     y_t[c] = (sum_n C_t[n] h_t[c][n] + D[c] x_t[c]) silu(z_t[c])   (z = NULL: without the last factor)
  * i.e. a node's first token continues from the end state of its PARENT node, as in tt_tree_gdn_fwd, and
  * by the same chunk program: chunk_tok0, chunk_len, chunk_src, chunk_dst, chunk_cap of tt_tree_gdn_plan
- * (device copies; chunk_cap may be NULL = nothing captured).  The forward takes chunks of any length,
- * the backward at most TT_GDN_CHUNK tokens (what lies behind them in a longer chunk is not computed).
+ * (device copies; chunk_cap may be NULL = nothing captured).  The forward takes chunks of at most
+ * TT_SCAN_CHUNK_MAX tokens, the backward of at most TT_GDN_CHUNK (what lies behind them in a longer chunk
+ * is not computed).
  * tt_tree_scan_join (host): the program with the chunks of one run joined as far as the forward is the
  *   faster for it with this many channels: arrays of n_chunks entries, *n_joined of them written (cap may
  *   be NULL).  The results are those of the program itself up to rounding.
  *   x, dt, z, y, dy [n_tokens][channels], b, c [n_tokens][groups][n_state], dtype bf16 or fp32, token
- *   strides in elements (0 = contiguous); A [channels][n_state] (rates, negative), D, dt_bias [channels]
+ *   strides in elements (0 = contiguous, below 2^19); A [channels][n_state] (rates, negative), D, dt_bias [channels]
  *   or NULL (= 0), fp32; n_state 4, 8 or 16; groups divides channels, and with several groups
  *   channels / groups is a multiple of 64.  States fp32: initial_state [channels][n_state] or NULL (= 0),
  *   state_out [n_capture][channels][n_state], given exactly when chunk_cap is.
@@ -716,7 +717,7 @@ tt_status tt_tree_gdn_bwd(int64_t n_tokens, int32_t hk, int32_t hv, int32_t dk, 
  *   TT_ERR_WORKSPACE; the workspace functions return 0 for an invalid descriptor.
  * ------------------------------------------------------------------------------------------ */
 #define TT_SCAN_CHUNK_MAX 1024      /* most tokens of a joined chunk                                       */
-#define TT_SCAN_MIN_WAVES 12288     /* chunks times blocks of 64 channels below which none are joined further */
+#define TT_SCAN_MIN_WAVES 12288   /* chunks times blocks of 64 channels below which none are joined further */
 typedef struct {
   int64_t n_tokens;
   int32_t channels, n_state, groups;

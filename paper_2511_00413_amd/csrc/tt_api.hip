@@ -653,7 +653,7 @@ tt_status check_scan_desc(const tt_scan_desc* in, tt_scan_desc& d) {
   d = *in;
   if (d.dtype != TT_DTYPE_BF16 && d.dtype != TT_DTYPE_FP32) return fail(TT_ERR_DTYPE, "unknown dtype %d", d.dtype);
   if (d.n_tokens < 0 || d.n_tokens >= INT32_MAX) return fail(TT_ERR_SHAPE, "n_tokens=%lld out of range", (long long)d.n_tokens);
-  if (d.channels <= 0 || d.channels > (1 << 20)) return fail(TT_ERR_SHAPE, "channels=%d must lie in [1, %d]", d.channels, 1 << 20);
+  if (d.channels <= 0 || d.channels >= (1 << 19)) return fail(TT_ERR_SHAPE, "channels=%d must lie in [1, %d]", d.channels, (1 << 19) - 1);
   if (d.n_state != 4 && d.n_state != 8 && d.n_state != 16) return fail(TT_ERR_UNSUPPORTED, "n_state=%d: 4, 8 and 16 are built", d.n_state);
   if (d.groups <= 0 || d.channels % d.groups) return fail(TT_ERR_SHAPE, "groups=%d must divide channels=%d", d.groups, d.channels);
   if (d.groups > 1 && d.channels / d.groups % 64)
@@ -664,6 +664,9 @@ tt_status check_scan_desc(const tt_scan_desc* in, tt_scan_desc& d) {
     if (*s == 0) *s = c;
     if (*s < c) return fail(TT_ERR_SHAPE, "token stride %lld is smaller than channels=%lld", (long long)*s, (long long)c);
   }
+  const int64_t most = (1 << 19) - 1;             // a chunk's rows are addressed by 32-bit byte counts
+  for (int64_t s : {d.x_stride_tok, d.dt_stride_tok, d.z_stride_tok, d.y_stride_tok, d.b_stride_tok, d.c_stride_tok})
+    if (s > most) return fail(TT_ERR_SHAPE, "token stride %lld is larger than %lld", (long long)s, (long long)most);
   for (int64_t* s : {&d.b_stride_tok, &d.c_stride_tok}) {
     if (*s == 0) *s = bc;
     if (*s < bc) return fail(TT_ERR_SHAPE, "token stride %lld is smaller than groups * n_state=%lld", (long long)*s, (long long)bc);
@@ -724,7 +727,7 @@ extern "C" size_t tt_tree_scan_bwd_workspace(const tt_scan_desc* desc, int32_t n
   tt::clear_error();
   tt_scan_desc d;
   if (check_scan_desc(desc, d) || n_chunks < 0 || n_slots < 0) return 0;
-  return tt::scan_bwd_workspace(d.n_tokens, d.channels, d.n_state, d.groups, n_chunks, n_slots);
+  return tt::scan_bwd_workspace(d.n_tokens, d.channels, d.n_state, n_chunks, n_slots);
 }
 
 extern "C" tt_status tt_tree_scan_fwd(const tt_scan_desc* desc, const tt_scan_chunks* chunks, const void* x, const void* dt,
@@ -786,7 +789,7 @@ extern "C" tt_status tt_tree_scan_bwd(const tt_scan_desc* desc, const tt_scan_ch
     for (const Span& p : outs)
       if (&p != &o && meets(o, p)) return fail(TT_ERR_SHAPE, "two outputs share memory");
   }
-  const size_t need = tt::scan_bwd_workspace(n, d.channels, d.n_state, d.groups, chunks->n_chunks, chunks->n_slots);
+  const size_t need = tt::scan_bwd_workspace(n, d.channels, d.n_state, chunks->n_chunks, chunks->n_slots);
   if (!workspace || workspace_bytes < need || !tt::aligned16(workspace))
     return fail(TT_ERR_WORKSPACE, "scan backward needs %zu bytes of 16-byte aligned workspace, got %zu", need, workspace_bytes);
   tt::ScanArgs a = scan_args(d, *chunks);

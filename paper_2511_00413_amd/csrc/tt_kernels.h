@@ -178,7 +178,7 @@ struct ScanArgs {
 };
 size_t scan_fwd_workspace(int channels, int n_state, int n_chunks, int n_slots);
 hipError_t scan_fwd(const ScanArgs& a, hipStream_t st);
-size_t scan_bwd_workspace(int64_t n_tokens, int channels, int n_state, int groups, int n_chunks, int n_slots);
+size_t scan_bwd_workspace(int64_t n_tokens, int channels, int n_state, int n_chunks, int n_slots);
 hipError_t scan_bwd(const ScanArgs& a, hipStream_t st);
 
 // one token per row from saved states (tt_step.hip); strides in elements

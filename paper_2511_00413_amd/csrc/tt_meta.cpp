@@ -520,17 +520,27 @@ extern "C" tt_status tt_tree_gdn_plan(int32_t n_nodes, const int32_t* parent, co
 }
 
 namespace {
-// One chunk for every maximal run of chunks whose state stays on chip, cut where the run would pass max_tokens.
+// One chunk for every maximal run of chunks whose state stays on chip; a run of more than max_tokens is cut into as many chunks as
+// that needs, of about equal length.
 template <typename Emit>
 int32_t join_chunks(int32_t n_chunks, const int32_t* len, const int32_t* src, const int32_t* dst, const int32_t* cap, int64_t max_tokens,
                     Emit emit) {
   int32_t n = 0;
   for (int32_t c = 0; c < n_chunks;) {
-    int32_t e = c + 1;
-    int64_t tokens = len[c];
-    while (e < n_chunks && src[e] == -2 && dst[e - 1] < 0 && (!cap || cap[e - 1] < 0) && tokens + len[e] <= max_tokens) tokens += len[e++];
-    emit(n++, c, e, (int32_t)tokens);
-    c = e;
+    int32_t end = c + 1;
+    int64_t total = len[c];
+    while (end < n_chunks && src[end] == -2 && dst[end - 1] < 0 && (!cap || cap[end - 1] < 0)) total += len[end++];
+    const int64_t parts = (total + max_tokens - 1) / max_tokens;
+    int64_t before = 0;
+    for (int64_t part = 1; c < end; part++) {
+      const int64_t upto = part < parts ? total * part / parts : total;
+      int64_t tokens = len[c];
+      int32_t e = c + 1;
+      while (e < end && before + tokens + len[e] / 2 <= upto && tokens + len[e] <= max_tokens) tokens += len[e++];
+      emit(n++, c, e, (int32_t)tokens);
+      before += tokens;
+      c = e;
+    }
   }
   return n;
 }

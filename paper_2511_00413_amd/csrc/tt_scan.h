@@ -18,38 +18,40 @@ template <typename T> __device__ __forceinline__ T from_f(float v);
 template <> __device__ __forceinline__ __hip_bfloat16 from_f<__hip_bfloat16>(float v) { return __float2bfloat16(v); }
 template <> __device__ __forceinline__ float from_f<float>(float v) { return v; }
 
-// ln(1 + e) for e in [0, 1]: the logarithm of the rounded sum w = 1 + e, corrected by e / (w - 1) for what the rounding took
-// (Kahan), so that small steps keep their relative precision.
+// ln(1 + e) for e in [0, 1]: the logarithm of the rounded sum w, and what its rounding took, e - (w - 1) (exact), so that small
+// steps keep their relative precision.  (To first order the correction is divided by w; it is at most 2^-24, so that where w is
+// not 1 to many digits the result is not small and the division does not show.)
 __device__ __forceinline__ float log1p_unit(float e) {
-  const float w = 1.f + e, d = w - 1.f;
-  return d == 0.f ? e : LN2 * __builtin_amdgcn_logf(w) * (e * __builtin_amdgcn_rcpf(d));
+  const float w = 1.f + e;
+  return fmaf(LN2, __builtin_amdgcn_logf(w), e - (w - 1.f));
 }
 __device__ __forceinline__ float softplus(float r) { return fmaxf(r, 0.f) + log1p_unit(ex2(-LOG2E * fabsf(r))); }
-// its derivative, without the cancellation of 1 - exp(-softplus(r))
-__device__ __forceinline__ float sigmoid(float r) {
-  const float e = ex2(-LOG2E * fabsf(r)), q = __builtin_amdgcn_rcpf(1.f + e);
-  return r >= 0.f ? q : e * q;
+// softplus or the value itself, by a selection (a branch here cuts the loops into pieces that the loads cannot be moved across)
+__device__ __forceinline__ float step_size(float r, bool use_softplus) {
+  float s = softplus(r);
+  asm volatile("" : "+v"(s));
+  return use_softplus ? s : r;
 }
+// its derivative (0 where the exponential is past fp32), without the cancellation of 1 - exp(-softplus(r))
+__device__ __forceinline__ float sigmoid(float r) { return __builtin_amdgcn_rcpf(1.f + ex2(-LOG2E * r)); }
 
-// A vector of NS inputs B or outputs C of one token, the same for all lanes: read through the scalar cache, so that its
-// elements are scalar operands.
-template <typename T, int NS>
-__device__ __forceinline__ void load_uniform(const T* p, float (&v)[NS]) {
+// A vector B or C of one token and group is the same for all lanes: read through the scalar cache, its elements are scalar operands.
+template <int N, typename T>
+__device__ __forceinline__ void load_uniform(const T* p, float (&v)[N]) {
   typedef const __attribute__((address_space(4))) uint32_t* Words;
   const Words w = (Words)(uintptr_t)p;
   if constexpr (sizeof(T) == 2) {
 #pragma unroll
-    for (int i = 0; i < NS / 2; i++) {
+    for (int i = 0; i < N / 2; i++) {
       const uint32_t q = w[i];
       v[2 * i] = __uint_as_float(q << 16);
       v[2 * i + 1] = __uint_as_float(q & 0xffff0000u);
     }
   } else {
 #pragma unroll
-    for (int i = 0; i < NS; i++) v[i] = __uint_as_float(w[i]);
+    for (int i = 0; i < N; i++) v[i] = __uint_as_float(w[i]);
   }
 }
-
 template <int NS>
 __device__ __forceinline__ void load_rates(const float* A, int64_t c, float (&a2)[NS]) {      // rates in base 2
 #pragma unroll
@@ -59,6 +61,162 @@ __device__ __forceinline__ void load_rates(const float* A, int64_t c, float (&a2
 // Whether anything starts from the state that chunk u leaves.
 __device__ __forceinline__ bool state_is_used(const ScanArgs& a, int u) {
   return a.chunk_dst[u] >= 0 || (a.chunk_cap && a.chunk_cap[u] >= 0) || (u + 1 < a.n_chunks && a.chunk_src[u + 1] == -2);
+}
+
+constexpr int THREADS = 256;
+constexpr int AHEAD = 4;                   // tokens whose loads are in flight behind the ones worked on
+
+// Workgroup `block` of a grid of chunks x channel blocks.
+struct Place { int chunk, c; bool valid; int64_t cc; int group; };
+__device__ __forceinline__ Place place(const ScanArgs& a, int blocks) {
+  Place p;
+  p.chunk = blockIdx.x / (unsigned)blocks;
+  p.c = (int)(blockIdx.x % (unsigned)blocks) * THREADS + threadIdx.x;
+  p.valid = p.c < a.channels;
+  p.cc = p.valid ? p.c : a.channels - 1;
+  p.group = __builtin_amdgcn_readfirstlane((int)p.cc) / (a.channels / a.groups);     // a wave's channels are of one group
+  return p;
+}
+
+// Rows of a chunk, one element per lane: buffer accesses, whose address is a scalar base, the lane's 32-bit offset and a scalar row
+// offset that one addition steps.  (As pointers, the multiples of every stride are worked out ahead of the loops and spilled, and
+// each access costs a 64-bit vector addition.)  A row offset stays below 2^31: strides are below 2^19 elements, chunks of at most
+// TT_SCAN_CHUNK_MAX = 2^10 rows.
+template <typename T>
+struct Feed {
+  __amdgpu_buffer_rsrc_t r;
+  int step, so;
+  __device__ __forceinline__ Feed(const void* base, int64_t stride, int64_t row0, int row = 0)
+      : r(__builtin_amdgcn_make_buffer_rsrc((char*)const_cast<void*>(base) + row0 * stride * (int64_t)sizeof(T), (short)0, -1, 0x00020000)),
+        step((int)stride * (int)sizeof(T)), so(row * ((int)stride * (int)sizeof(T))) {}
+  // the lane's element of this row, then on to the next row if `more`
+  __device__ __forceinline__ T next(uint32_t lane_bytes, bool more) {
+    T v;
+    if constexpr (sizeof(T) == 2) v = __builtin_bit_cast(T, __builtin_amdgcn_raw_buffer_load_b16(r, lane_bytes, so, 0));
+    else v = __builtin_bit_cast(T, __builtin_amdgcn_raw_buffer_load_b32(r, lane_bytes, so, 0));
+    so += more ? step : 0;
+    return v;
+  }
+  __device__ __forceinline__ void put(uint32_t lane_bytes, float f) {
+    const T v = from_f<T>(f);
+    if constexpr (sizeof(T) == 2) __builtin_amdgcn_raw_buffer_store_b16(__builtin_bit_cast(unsigned short, v), r, lane_bytes, so, 0);
+    else __builtin_amdgcn_raw_buffer_store_b32(__builtin_bit_cast(unsigned int, v), r, lane_bytes, so, 0);
+  }
+};
+// vectors of rows that are the same for all lanes
+template <typename T>
+struct UniformFeed {
+  const char* p;
+  int step;
+  __device__ __forceinline__ UniformFeed(const void* base, int64_t stride, int64_t row0, int at)
+      : p((const char*)base + (row0 * stride + at) * (int64_t)sizeof(T)), step((int)stride * (int)sizeof(T)) {}
+  template <int N>
+  __device__ __forceinline__ void next(float (&v)[N]) {
+    load_uniform<N>((const T*)p, v);
+    p += step;
+  }
+  template <int N>
+  __device__ __forceinline__ void prev(float (&v)[N]) {
+    load_uniform<N>((const T*)p, v);
+    p -= step;
+  }
+};
+
+// Tokens 0 .. len in blocks of AHEAD, the loads of a block issued before the one in front of it is worked on.
+template <typename In, typename Request, typename Work>
+__device__ __forceinline__ void stream(int len, Request request, Work work) {
+  In buf[2][AHEAD];
+  request(0, buf[0]);
+  int t = 0;
+  for (; t + 2 * AHEAD <= len; t += 2 * AHEAD) {
+    request(t + AHEAD, buf[1]);
+#pragma unroll
+    for (int j = 0; j < AHEAD; j++) work(t + j, buf[0][j]);
+    request(t + 2 * AHEAD, buf[0]);
+#pragma unroll
+    for (int j = 0; j < AHEAD; j++) work(t + AHEAD + j, buf[1][j]);
+  }
+  if (t + AHEAD <= len) {
+    request(t + AHEAD, buf[1]);
+#pragma unroll
+    for (int j = 0; j < AHEAD; j++) work(t + j, buf[0][j]);
+    t += AHEAD;
+#pragma unroll
+    for (int j = 0; j < AHEAD; j++) buf[0][j] = buf[1][j];
+  }
+#pragma unroll
+  for (int j = 0; j < AHEAD; j++)
+    if (t + j < len) work(t + j, buf[0][j]);
+}
+
+// The walks along the chunk program (one lane per channel and state): what a chunk contributes does not depend on the walk, so a
+// block of WALK chunks is requested before the one in front of it is walked, and its results are stored in one go behind it: no
+// branch lies between a load and its use, where the wait for it would become a wait for everything.  The program's entries come 64
+// at a time, a lane each.
+constexpr int WALK = 16;
+constexpr int WALK_THREADS = 256;
+constexpr int LDS_SLOTS = 64;                   // saved states held in LDS: up to 64 KB a workgroup; more live in the workspace
+struct Program {
+  int src, dst, cap;
+  __device__ __forceinline__ void load(const ScanArgs& a, int base, bool with_cap) {
+    const int u = min(base + (int)(threadIdx.x & 63), a.n_chunks - 1);
+    src = a.chunk_src[u];
+    dst = a.chunk_dst[u];
+    cap = with_cap ? a.chunk_cap[u] : -1;
+  }
+  static __device__ __forceinline__ int at(int v, int u) { return __builtin_amdgcn_readlane(v, u & 63); }
+};
+template <bool LDS>
+struct Slots {
+  float* p;
+  int64_t step;
+  __device__ __forceinline__ Slots(float* lds, float* global, int64_t width, int64_t at)
+      : p(LDS ? lds + threadIdx.x : global + at), step(LDS ? WALK_THREADS : width) {}
+  __device__ __forceinline__ float& operator[](int s) const { return p[s * step]; }
+};
+
+// Down the tree: replaces add[chunk] by the state entering the chunk.  leave(cap, state) sees the captured states.
+// (Lanes past the last entry stand in for it: they write what it writes.)
+template <bool LDS, typename Leave>
+__device__ __forceinline__ void walk_down(const ScanArgs& a, float* local, const float* __restrict__ steps, int64_t width, int64_t at, int c,
+                                          float a2, float first, const Slots<LDS>& slots, bool with_cap, Leave leave) {
+  Program prog;
+  float s = first, add[2][WALK], len[2][WALK];
+  auto request = [&](int u0, float (&h)[WALK], float (&d)[WALK]) {
+#pragma unroll
+    for (int j = 0; j < WALK; j++) {
+      const int64_t u = min(u0 + j, a.n_chunks - 1);
+      h[j] = local[u * width + at];
+      d[j] = steps[u * a.channels + c];
+    }
+  };
+  auto walk = [&](int u0, const float (&h)[WALK], const float (&d)[WALK]) {
+    float entering[WALK];
+#pragma unroll
+    for (int j = 0; j < WALK; j++) {
+      const int u = u0 + j;
+      if (u < a.n_chunks) {
+        const int src = Program::at(prog.src, u), dst = Program::at(prog.dst, u), cap = Program::at(prog.cap, u);
+        if (src == -1) s = first;
+        else if (src >= 0) s = slots[src];
+        entering[j] = s;
+        s = fmaf(ex2(d[j] * a2), s, h[j]);
+        if (dst >= 0) slots[dst] = s;
+        if (cap >= 0) leave(cap, s);
+      }
+    }
+#pragma unroll
+    for (int j = 0; j < WALK; j++)
+      if (u0 + j < a.n_chunks) local[(int64_t)(u0 + j) * width + at] = entering[j];
+  };
+  request(0, add[0], len[0]);
+  for (int u0 = 0; u0 < a.n_chunks; u0 += 2 * WALK) {
+    if (u0 % 64 == 0) prog.load(a, u0, with_cap);
+    if (u0 + WALK < a.n_chunks) request(u0 + WALK, add[1], len[1]);
+    walk(u0, add[0], len[0]);
+    if (u0 + 2 * WALK < a.n_chunks) request(u0 + 2 * WALK, add[0], len[0]);
+    walk(u0 + WALK, add[1], len[1]);
+  }
 }
 
 template <typename F>

@@ -20,64 +20,40 @@ namespace tt {
 namespace {
 using namespace scan;
 
-constexpr int THREADS = 256;
-constexpr int AHEAD = 4;                   // tokens whose loads are in flight behind the ones worked on
-
-// Workgroup `block` of a grid of chunks x channel blocks.
-struct Place { int chunk, c; bool valid; int64_t cc; int group; };
-__device__ __forceinline__ Place place(const ScanArgs& a, int blocks) {
-  Place p;
-  p.chunk = blockIdx.x / (unsigned)blocks;
-  p.c = (int)(blockIdx.x % (unsigned)blocks) * THREADS + threadIdx.x;
-  p.valid = p.c < a.channels;
-  p.cc = p.valid ? p.c : a.channels - 1;
-  p.group = __builtin_amdgcn_readfirstlane((int)p.cc / (a.channels / a.groups));     // a wave's channels are of one group
-  return p;
-}
-
 template <typename T, int NS>
 __global__ void __launch_bounds__(THREADS)
 scan_carry_kernel(ScanArgs a, int blocks, float* __restrict__ local, float* __restrict__ steps) {
   const Place p = place(a, blocks);
+  const int t0 = a.chunk_tok0[p.chunk], len = min(a.chunk_len[p.chunk], TT_SCAN_CHUNK_MAX);
   if (!state_is_used(a, p.chunk)) return;
-  const int t0 = a.chunk_tok0[p.chunk], len = a.chunk_len[p.chunk];
-  const T* x = (const T*)a.x + (int64_t)t0 * a.x_stride;
-  const T* dt = (const T*)a.dt + (int64_t)t0 * a.dt_stride;
-  const T* b = (const T*)a.b + (int64_t)t0 * a.b_stride + p.group * NS;
+  Feed<T> x(a.x, a.x_stride, t0), dt(a.dt, a.dt_stride, t0);
+  UniformFeed<T> b(a.b, a.b_stride, t0, p.group * NS);
   float a2[NS], h[NS], total = 0.f;
   load_rates<NS>(a.A, p.cc, a2);
 #pragma unroll
   for (int n = 0; n < NS; n++) h[n] = 0.f;
   const float bias = a.dt_bias ? a.dt_bias[p.cc] : 0.f;
-  T xs[2][AHEAD], ds[2][AHEAD];
-  auto request = [&](int t, T (&xv)[AHEAD], T (&dv)[AHEAD]) {
+  const uint32_t off = (uint32_t)p.cc * sizeof(T);
+  struct In { T x, dt; };
+  stream<In>(
+      len,
+      [&](int t, In (&v)[AHEAD]) {
 #pragma unroll
-    for (int j = 0; j < AHEAD; j++) {
-      const int64_t s = min(t + j, len - 1);
-      xv[j] = (x + s * a.x_stride)[p.cc];
-      dv[j] = (dt + s * a.dt_stride)[p.cc];
-    }
-  };
-  auto work = [&](int t, const T (&xv)[AHEAD], const T (&dv)[AHEAD]) {
+        for (int j = 0; j < AHEAD; j++) {
+          const bool more = t + j < len - 1;
+          v[j].x = x.next(off, more);
+          v[j].dt = dt.next(off, more);
+        }
+      },
+      [&](int, const In& v) {
+        float bv[NS];
+        b.next(bv);
+        const float raw = to_f(v.dt) + bias, delta = step_size(raw, a.use_softplus);
+        const float u = delta * to_f(v.x);
+        total += delta;
 #pragma unroll
-    for (int j = 0; j < AHEAD; j++) {
-      if (t + j >= len) break;
-      float bv[NS];
-      load_uniform<T, NS>(b + (int64_t)(t + j) * a.b_stride, bv);
-      const float raw = to_f(dv[j]) + bias, delta = a.use_softplus ? softplus(raw) : raw;
-      const float u = delta * to_f(xv[j]);
-      total += delta;
-#pragma unroll
-      for (int n = 0; n < NS; n++) h[n] = fmaf(ex2(delta * a2[n]), h[n], u * bv[n]);
-    }
-  };
-  request(0, xs[0], ds[0]);
-  for (int t = 0; t < len; t += 2 * AHEAD) {
-    request(t + AHEAD, xs[1], ds[1]);
-    work(t, xs[0], ds[0]);
-    request(t + 2 * AHEAD, xs[0], ds[0]);
-    work(t + AHEAD, xs[1], ds[1]);
-  }
+        for (int n = 0; n < NS; n++) h[n] = fmaf(ex2(delta * a2[n]), h[n], u * bv[n]);
+      });
   if (!p.valid) return;
   float* out = local + (int64_t)p.chunk * NS * a.channels + p.c;
 #pragma unroll
@@ -86,97 +62,64 @@ scan_carry_kernel(ScanArgs a, int blocks, float* __restrict__ local, float* __re
 }
 
 // One lane per (state, channel) walks the chunk program.  local[chunk] is replaced by the chunk's entering state.
-// What a chunk contributes does not depend on the walk, so it is requested WALK chunks ahead.
-constexpr int WALK = 8;
-__global__ void __launch_bounds__(THREADS)
-scan_states_kernel(ScanArgs a, float* local, const float* __restrict__ steps, float* slots) {
+template <bool LDS>
+__global__ void __launch_bounds__(WALK_THREADS)
+scan_states_kernel(ScanArgs a, float* local, const float* __restrict__ steps, float* saved) {
+  extern __shared__ float lds[];
   const int64_t width = (int64_t)a.n_state * a.channels;
-  const int64_t at = (int64_t)blockIdx.x * THREADS + threadIdx.x;
-  if (at >= width) return;
+  const int64_t at = min((int64_t)blockIdx.x * WALK_THREADS + threadIdx.x, width - 1);
   const int n = (int)(at / a.channels), c = (int)(at - (int64_t)n * a.channels);
-  const float a2 = a.A[(int64_t)c * a.n_state + n] * LOG2E;
-  const float first = a.initial_state ? a.initial_state[(int64_t)c * a.n_state + n] : 0.f;
-  float s = first, add[WALK], len[WALK];
-  auto request = [&](int u, float& h, float& d) {
-    u = min(u, a.n_chunks - 1);
-    h = local[u * width + at];
-    d = steps[(int64_t)u * a.channels + c];
-  };
-#pragma unroll
-  for (int j = 0; j < WALK; j++) request(j, add[j], len[j]);
-  for (int u0 = 0; u0 < a.n_chunks; u0 += WALK) {
-#pragma unroll
-    for (int j = 0; j < WALK; j++) {
-      const int u = u0 + j;
-      if (u >= a.n_chunks) break;
-      const int src = a.chunk_src[u], dst = a.chunk_dst[u], cap = a.chunk_cap ? a.chunk_cap[u] : -1;
-      if (src == -1) s = first;
-      else if (src >= 0) s = slots[src * width + at];
-      local[u * width + at] = s;
-      s = fmaf(ex2(len[j] * a2), s, add[j]);
-      if (dst >= 0) slots[dst * width + at] = s;
-      if (cap >= 0) a.state_out[((int64_t)cap * a.channels + c) * a.n_state + n] = s;
-      if (u + WALK < a.n_chunks) request(u + WALK, add[j], len[j]);
-    }
-  }
+  const int64_t state_at = (int64_t)c * a.n_state + n;
+  const Slots<LDS> slots(lds, saved, width, at);
+  walk_down<LDS>(a, local, steps, width, at, c, a.A[state_at] * LOG2E, a.initial_state ? a.initial_state[state_at] : 0.f, slots,
+                 a.chunk_cap != nullptr, [&](int cap, float s) { a.state_out[cap * width + state_at] = s; });
 }
 
 template <typename T, int NS, bool GATED>
 __global__ void __launch_bounds__(THREADS)
 scan_out_kernel(ScanArgs a, int blocks, const float* __restrict__ states) {
   const Place p = place(a, blocks);
-  const int t0 = a.chunk_tok0[p.chunk], len = a.chunk_len[p.chunk];
-  const T* x = (const T*)a.x + (int64_t)t0 * a.x_stride;
-  const T* dt = (const T*)a.dt + (int64_t)t0 * a.dt_stride;
-  const T* z = GATED ? (const T*)a.z + (int64_t)t0 * a.z_stride : nullptr;
-  const T* b = (const T*)a.b + (int64_t)t0 * a.b_stride + p.group * NS;
-  const T* c = (const T*)a.c + (int64_t)t0 * a.c_stride + p.group * NS;
-  T* y = (T*)a.y + (int64_t)t0 * a.y_stride;
+  const int t0 = a.chunk_tok0[p.chunk], len = min(a.chunk_len[p.chunk], TT_SCAN_CHUNK_MAX);
+  Feed<T> x(a.x, a.x_stride, t0), dt(a.dt, a.dt_stride, t0), z(a.z, a.z_stride, t0);
+  UniformFeed<T> b(a.b, a.b_stride, t0, p.group * NS), c(a.c, a.c_stride, t0, p.group * NS);
+  Feed<T> y(a.y, a.y_stride, t0);
   float a2[NS], h[NS];
   load_rates<NS>(a.A, p.cc, a2);
 #pragma unroll
   for (int n = 0; n < NS; n++) h[n] = states[((int64_t)p.chunk * NS + n) * a.channels + p.cc];
   const float bias = a.dt_bias ? a.dt_bias[p.cc] : 0.f, skip = a.D ? a.D[p.cc] : 0.f;
+  const uint32_t off = (uint32_t)p.cc * sizeof(T);
   struct In { T x, dt, z; };
-  In buf[2][AHEAD];
-  auto request = [&](int t, In (&v)[AHEAD]) {
+  stream<In>(
+      len,
+      [&](int t, In (&v)[AHEAD]) {
 #pragma unroll
-    for (int j = 0; j < AHEAD; j++) {
-      const int64_t s = min(t + j, len - 1);
-      v[j].x = (x + s * a.x_stride)[p.cc];
-      v[j].dt = (dt + s * a.dt_stride)[p.cc];
-      if constexpr (GATED) v[j].z = (z + s * a.z_stride)[p.cc];
-    }
-  };
-  auto work = [&](int t, const In (&v)[AHEAD]) {
+        for (int j = 0; j < AHEAD; j++) {
+          const bool more = t + j < len - 1;
+          v[j].x = x.next(off, more);
+          v[j].dt = dt.next(off, more);
+          if constexpr (GATED) v[j].z = z.next(off, more);
+        }
+      },
+      [&](int, const In& v) {
+        float bv[NS], cv[NS];
+        b.next(bv);
+        c.next(cv);
+        const float raw = to_f(v.dt) + bias, delta = step_size(raw, a.use_softplus);
+        const float xv = to_f(v.x), u = delta * xv;
+        float out = skip * xv;
 #pragma unroll
-    for (int j = 0; j < AHEAD; j++) {
-      if (t + j >= len) break;
-      float bv[NS], cv[NS];
-      load_uniform<T, NS>(b + (int64_t)(t + j) * a.b_stride, bv);
-      load_uniform<T, NS>(c + (int64_t)(t + j) * a.c_stride, cv);
-      const float raw = to_f(v[j].dt) + bias, delta = a.use_softplus ? softplus(raw) : raw;
-      const float xv = to_f(v[j].x), u = delta * xv;
-      float out = skip * xv;
-#pragma unroll
-      for (int n = 0; n < NS; n++) {
-        h[n] = fmaf(ex2(delta * a2[n]), h[n], u * bv[n]);
-        out = fmaf(cv[n], h[n], out);
-      }
-      if constexpr (GATED) {
-        const float zv = to_f(v[j].z);
-        out *= zv * sigmoid(zv);
-      }
-      if (p.valid) (y + (int64_t)(t + j) * a.y_stride)[p.c] = from_f<T>(out);
-    }
-  };
-  request(0, buf[0]);
-  for (int t = 0; t < len; t += 2 * AHEAD) {
-    request(t + AHEAD, buf[1]);
-    work(t, buf[0]);
-    request(t + 2 * AHEAD, buf[0]);
-    work(t + AHEAD, buf[1]);
-  }
+        for (int n = 0; n < NS; n++) {
+          h[n] = fmaf(ex2(delta * a2[n]), h[n], u * bv[n]);
+          out = fmaf(cv[n], h[n], out);
+        }
+        if constexpr (GATED) {
+          const float zv = to_f(v.z);
+          out *= zv * sigmoid(zv);
+        }
+        if (p.valid) y.put(off, out);
+        y.so += y.step;
+      });
 }
 
 size_t up(size_t v) { return (v + 255) & ~(size_t)255; }
@@ -206,7 +149,10 @@ hipError_t scan_fwd(const ScanArgs& a, hipStream_t st) {
     if (hipError_t e = hipGetLastError()) return e;
     {
       KernelTimer timer(TT_KERNEL_SCAN_STATES, st);
-      scan_states_kernel<<<(unsigned)((NS * (int64_t)a.channels + THREADS - 1) / THREADS), THREADS, 0, st>>>(a, local, steps, slots);
+      const unsigned walkers = (unsigned)((NS * (int64_t)a.channels + WALK_THREADS - 1) / WALK_THREADS);
+      const size_t lds = (size_t)a.n_slots * WALK_THREADS * sizeof(float);
+      if (a.n_slots <= LDS_SLOTS) scan_states_kernel<true><<<walkers, WALK_THREADS, lds, st>>>(a, local, steps, slots);
+      else scan_states_kernel<false><<<walkers, WALK_THREADS, 0, st>>>(a, local, steps, slots);
     }
     if (hipError_t e = hipGetLastError()) return e;
     KernelTimer timer(TT_KERNEL_SCAN_OUT, st);

@@ -8,7 +8,6 @@ namespace tt {
 namespace {
 using namespace scan;
 
-constexpr int THREADS = 256;
 
 template <typename T> struct alignas(4 * sizeof(T)) Four { T v[4]; };
 
