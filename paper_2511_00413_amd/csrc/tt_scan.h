@@ -36,22 +36,22 @@ __device__ __forceinline__ float step_size(float r, bool use_softplus) {
 __device__ __forceinline__ float sigmoid(float r) { return __builtin_amdgcn_rcpf(1.f + ex2(-LOG2E * r)); }
 
 // A vector B or C of one token and group is the same for all lanes: read through the scalar cache, its elements are scalar operands.
-template <int N, typename T>
-__device__ __forceinline__ void load_uniform(const T* p, float (&v)[N]) {
-  typedef const __attribute__((address_space(4))) uint32_t* Words;
-  const Words w = (Words)(uintptr_t)p;
-  if constexpr (sizeof(T) == 2) {
+template <typename T, int N>
+struct Words {                                  // as they lie in memory: bf16 in pairs
+  static constexpr int W = N * (int)sizeof(T) / 4;
+  uint32_t w[W];
+  __device__ __forceinline__ void load(const void* p) {
+    typedef const __attribute__((address_space(4))) uint32_t* Scalar;
+    const Scalar q = (Scalar)(uintptr_t)p;
 #pragma unroll
-    for (int i = 0; i < N / 2; i++) {
-      const uint32_t q = w[i];
-      v[2 * i] = __uint_as_float(q << 16);
-      v[2 * i + 1] = __uint_as_float(q & 0xffff0000u);
-    }
-  } else {
-#pragma unroll
-    for (int i = 0; i < N; i++) v[i] = __uint_as_float(w[i]);
+    for (int i = 0; i < W; i++) w[i] = q[i];
   }
-}
+  __device__ __forceinline__ float operator[](int i) const {
+    if constexpr (sizeof(T) == 2) return __uint_as_float(i & 1 ? w[i / 2] & 0xffff0000u : w[i / 2] << 16);
+    else return __uint_as_float(w[i]);
+  }
+};
+
 template <int NS>
 __device__ __forceinline__ void load_rates(const float* A, int64_t c, float (&a2)[NS]) {      // rates in base 2
 #pragma unroll
@@ -104,22 +104,14 @@ struct Feed {
   }
 };
 // vectors of rows that are the same for all lanes
-template <typename T>
+template <typename T, int N>
 struct UniformFeed {
   const char* p;
   int step;
-  __device__ __forceinline__ UniformFeed(const void* base, int64_t stride, int64_t row0, int at)
-      : p((const char*)base + (row0 * stride + at) * (int64_t)sizeof(T)), step((int)stride * (int)sizeof(T)) {}
-  template <int N>
-  __device__ __forceinline__ void next(float (&v)[N]) {
-    load_uniform<N>((const T*)p, v);
-    p += step;
-  }
-  template <int N>
-  __device__ __forceinline__ void prev(float (&v)[N]) {
-    load_uniform<N>((const T*)p, v);
-    p -= step;
-  }
+  __device__ __forceinline__ UniformFeed(const void* base, int64_t stride, int64_t row, int at)
+      : p((const char*)base + (row * stride + at) * (int64_t)sizeof(T)), step((int)stride * (int)sizeof(T)) {}
+  __device__ __forceinline__ void next(Words<T, N>& v) { v.load(p); p += step; }
+  __device__ __forceinline__ void prev(Words<T, N>& v) { v.load(p); p -= step; }
 };
 
 // Tokens 0 .. len in blocks of AHEAD, the loads of a block issued before the one in front of it is worked on.

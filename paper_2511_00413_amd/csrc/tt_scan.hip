@@ -27,7 +27,7 @@ scan_carry_kernel(ScanArgs a, int blocks, float* __restrict__ local, float* __re
   const int t0 = a.chunk_tok0[p.chunk], len = min(a.chunk_len[p.chunk], TT_SCAN_CHUNK_MAX);
   if (!state_is_used(a, p.chunk)) return;
   Feed<T> x(a.x, a.x_stride, t0), dt(a.dt, a.dt_stride, t0);
-  UniformFeed<T> b(a.b, a.b_stride, t0, p.group * NS);
+  UniformFeed<T, NS> b(a.b, a.b_stride, t0, p.group * NS);
   float a2[NS], h[NS], total = 0.f;
   load_rates<NS>(a.A, p.cc, a2);
 #pragma unroll
@@ -46,7 +46,7 @@ scan_carry_kernel(ScanArgs a, int blocks, float* __restrict__ local, float* __re
         }
       },
       [&](int, const In& v) {
-        float bv[NS];
+        Words<T, NS> bv;
         b.next(bv);
         const float raw = to_f(v.dt) + bias, delta = step_size(raw, a.use_softplus);
         const float u = delta * to_f(v.x);
@@ -81,7 +81,7 @@ scan_out_kernel(ScanArgs a, int blocks, const float* __restrict__ states) {
   const Place p = place(a, blocks);
   const int t0 = a.chunk_tok0[p.chunk], len = min(a.chunk_len[p.chunk], TT_SCAN_CHUNK_MAX);
   Feed<T> x(a.x, a.x_stride, t0), dt(a.dt, a.dt_stride, t0), z(a.z, a.z_stride, t0);
-  UniformFeed<T> b(a.b, a.b_stride, t0, p.group * NS), c(a.c, a.c_stride, t0, p.group * NS);
+  UniformFeed<T, NS> b(a.b, a.b_stride, t0, p.group * NS), c(a.c, a.c_stride, t0, p.group * NS);
   Feed<T> y(a.y, a.y_stride, t0);
   float a2[NS], h[NS];
   load_rates<NS>(a.A, p.cc, a2);
@@ -102,7 +102,7 @@ scan_out_kernel(ScanArgs a, int blocks, const float* __restrict__ states) {
         }
       },
       [&](int, const In& v) {
-        float bv[NS], cv[NS];
+        Words<T, NS> bv, cv;
         b.next(bv);
         c.next(cv);
         const float raw = to_f(v.dt) + bias, delta = step_size(raw, a.use_softplus);

@@ -42,7 +42,7 @@ scan_ends_kernel(ScanArgs a, int blocks, float* __restrict__ local, float* __res
   const Place p = place(a, blocks);
   const int t0 = a.chunk_tok0[p.chunk], len = min(a.chunk_len[p.chunk], CHUNK);
   Feed<T> x(a.x, a.x_stride, t0), dt(a.dt, a.dt_stride, t0), z(a.z, a.z_stride, t0), dy(a.dy, a.dy_stride, t0);
-  UniformFeed<T> b(a.b, a.b_stride, t0, p.group * NS), c(a.c, a.c_stride, t0, p.group * NS);
+  UniformFeed<T, NS> b(a.b, a.b_stride, t0, p.group * NS), c(a.c, a.c_stride, t0, p.group * NS);
   float a2[NS], h[NS], along[NS], r[NS], total = 0.f;
   load_rates<NS>(a.A, p.cc, a2);
 #pragma unroll
@@ -70,7 +70,7 @@ scan_ends_kernel(ScanArgs a, int blocks, float* __restrict__ local, float* __res
           for (int n = 0; n < NS; n++, out.so += out.step) out.put((uint32_t)p.c * 4u, h[n]);
           front_steps[f * a.channels + p.c] = total;
         }
-        float bv[NS], cv[NS];
+        Words<T, NS> bv, cv;
         b.next(bv);
         c.next(cv);
         const float raw = to_f(v.dt) + bias, delta = step_size(raw, a.use_softplus);
@@ -110,14 +110,18 @@ scan_bwd_states_kernel(ScanArgs a, float* local, float* back, const float* __res
   const int n = (int)(at / a.channels), c = (int)(at - (int64_t)n * a.channels);
   const int64_t state_at = (int64_t)c * a.n_state + n;
   if (a.n_chunks == 0) {
-    a.d_initial_state[state_at] = 0.f;
+    if (blockIdx.y) a.d_initial_state[state_at] = 0.f;
     return;
   }
-  const Slots<LDS> slots(lds, saved, width, at);
+  // the two walks do not depend on each other: one half of the workgroups takes the way down, the other the way up
+  const Slots<LDS> slots(lds, saved + (blockIdx.y ? a.n_slots * width : 0), width, at);
   const float a2 = a.A[state_at] * LOG2E;
-  walk_down<LDS>(a, local, steps, width, at, c, a2, a.initial_state ? a.initial_state[state_at] : 0.f, slots, false, [](int, float) {});
+  if (blockIdx.y == 0) {
+    walk_down<LDS>(a, local, steps, width, at, c, a2, a.initial_state ? a.initial_state[state_at] : 0.f, slots, false, [](int, float) {});
+    return;
+  }
   // up the tree: back[chunk] (the gradient of the entering state that the chunk's outputs give) becomes that of the leaving state
-  for (int s = 0; s < a.n_slots; s++) slots[s] = 0.f;                          // from here on: gradients of the saved states
+  for (int s = 0; s < a.n_slots; s++) slots[s] = 0.f;                          // gradients of the saved states
   const bool with_cap = a.d_state_out != nullptr;
   Program prog;
   float sent = 0.f, d_first = 0.f, add[2][WALK], len[2][WALK];
@@ -226,6 +230,8 @@ template <typename T, int NS, bool GATED>
 __global__ void __launch_bounds__(WAVE, 2)
 scan_grads_kernel(ScanArgs a, int blocks, int strips, GradBuffers buf) {
   __shared__ float4 entering[NS / 4][WAVE], before[NS / 4][WAVE];       // the chunk's entering state; the state in front of the SUB tokens
+  // the lanes that hold the same entry of the sums over the wave: one half of them stores its dB, the other its dC
+  constexpr int SHARE = WAVE / NS, HALF = SHARE / 2;
   struct In { T x, dt, z, dy; };
   __shared__ In inputs[SUB][WAVE];
   const int lane = threadIdx.x;
@@ -234,7 +240,7 @@ scan_grads_kernel(ScanArgs a, int blocks, int strips, GradBuffers buf) {
   const bool valid = ch < a.channels;
   const int cc = valid ? ch : a.channels - 1;
   const int group = __builtin_amdgcn_readfirstlane(cc / (a.channels / a.groups));
-  const uint32_t off = (uint32_t)cc * sizeof(T);
+  const uint32_t off = (uint32_t)cc * sizeof(T), bc_off = 4u * ((lane & HALF ? NS : 0) + lane / SHARE);
   float a2[NS], dA[NS], G[NS];
   load_rates<NS>(a.A, cc, a2);
 #pragma unroll
@@ -258,91 +264,103 @@ scan_grads_kernel(ScanArgs a, int blocks, int strips, GradBuffers buf) {
     for (int n = 0; n < NS; n++) h[n] = f.next((uint32_t)cc * 4u, true);
   };
   auto delta_of = [&](T raw) { return step_size(to_f(raw) + bias, a.use_softplus); };
-  auto step = [&](const float (&from)[NS], float (&h)[NS], const float (&bv)[NS], float delta, float u) {
+  auto step = [&](const float (&from)[NS], float (&h)[NS], const Words<T, NS>& bv, float delta, float u) {
 #pragma unroll
     for (int n = 0; n < NS; n++) h[n] = fmaf(ex2(delta * a2[n]), from[n], u * bv[n]);
   };
 
   for (int chunk = strip; chunk < a.n_chunks; chunk += strips) {
     const int t0 = __builtin_amdgcn_readfirstlane(a.chunk_tok0[chunk]), len = __builtin_amdgcn_readfirstlane(min(a.chunk_len[chunk], CHUNK));
+    Feed<float> bc(buf.bc, 2 * NS, (int64_t)block * a.n_tokens + t0);
     Feed<T> dx(a.dx, a.channels, t0), ddt(a.ddt, a.channels, t0), dz(a.dz, a.channels, t0);
     float h0[NS];
     per_state(buf.states, chunk, h0);
     per_state(buf.back, chunk, G);
     save(entering, h0);
 
+    // the inputs of SUB tokens and the state from zero in front of them
+    In in[SUB];
+    float from_zero[NS], along = 0.f;
+    auto request = [&](int s) {
+      const int base = s * SUB, m = min(SUB, len - base);
+      Feed<T> x(a.x, a.x_stride, t0, base), dt(a.dt, a.dt_stride, t0, base), z(a.z, a.z_stride, t0, base), dy(a.dy, a.dy_stride, t0, base);
+#pragma unroll
+      for (int j = 0; j < SUB; j++) {
+        const bool more = j < m - 1;
+        in[j].x = x.next(off, more);
+        in[j].dt = dt.next(off, more);
+        if constexpr (GATED) in[j].z = z.next(off, more);
+        in[j].dy = dy.next(off, more);
+      }
+      if (s) {
+        per_state(buf.fronts, front(t0, s), from_zero);
+        along = buf.front_steps[front(t0, s) * a.channels + cc];
+      }
+    };
+    request((len - 1) / SUB);
+
     for (int s = (len - 1) / SUB; s >= 0; s--) {
       const int base = s * SUB, m = min(SUB, len - base);
-      // the inputs of these tokens wait in LDS: with all their states in registers there is no room for them there
-      {
-        Feed<T> x(a.x, a.x_stride, t0, base), dt(a.dt, a.dt_stride, t0, base), z(a.z, a.z_stride, t0, base), dy(a.dy, a.dy_stride, t0, base);
-        In in[SUB];
+      // the inputs wait in LDS: with all states of these tokens in registers there is no room for them there
 #pragma unroll
-        for (int j = 0; j < SUB; j++) {
-          const bool more = j < m - 1;
-          in[j].x = x.next(off, more);
-          in[j].dt = dt.next(off, more);
-          if constexpr (GATED) in[j].z = z.next(off, more);
-          in[j].dy = dy.next(off, more);
-        }
-        restore(entering, h0);
-        if (s) {
-          float from_zero[NS];
-          per_state(buf.fronts, front(t0, s), from_zero);
-          const float along = buf.front_steps[front(t0, s) * a.channels + cc];
+      for (int j = 0; j < SUB; j++) inputs[j][lane] = in[j];
+      restore(entering, h0);
+      if (s)
 #pragma unroll
-          for (int n = 0; n < NS; n++) h0[n] = fmaf(ex2(along * a2[n]), h0[n], from_zero[n]);
-        }
-#pragma unroll
-        for (int j = 0; j < SUB; j++) {
-          if (!valid) in[j].x = in[j].dy = from_f<T>(0.f);
-          inputs[j][lane] = in[j];
-        }
-        save(before, h0);
-      }
+        for (int n = 0; n < NS; n++) h0[n] = fmaf(ex2(along * a2[n]), h0[n], from_zero[n]);
+      save(before, h0);
       float h[SUB][NS], delta[SUB];
-      UniformFeed<T> b(a.b, a.b_stride, t0 + base, group * NS);
+      UniformFeed<T, NS> b(a.b, a.b_stride, t0 + base, group * NS), c(a.c, a.c_stride, t0 + base + m - 1, group * NS);
 #pragma unroll
       for (int j = 0; j < SUB; j++) {
         if (j >= m) break;
-        float bv[NS];
+        Words<T, NS> bv;
         b.next(bv);
         delta[j] = delta_of(inputs[j][lane].dt);
         step(j ? h[j - 1] : h0, h[j], bv, delta[j], delta[j] * to_f(inputs[j][lane].x));
       }
-      UniformFeed<T> c(a.c, a.c_stride, t0 + base + m - 1, group * NS);
       b.p -= b.step;                             // both from the last token back
       asm volatile("" : "+s"(b.p));              // (the vectors kept from above would be spilled)
+      // the vectors of a token are requested while the one behind it is worked on
+      Words<T, NS> bv, cv, next_b, next_c;
+      b.prev(next_b);
+      c.prev(next_c);
+      // The next group is requested as soon as the states of half the tokens are used up: there its registers come from.
+      if (s && m <= SUB / 2) request(s - 1);
 #pragma unroll
       for (int j = SUB - 1; j >= 0; j--) {
         if (j >= m) continue;
-        const int t = base + j;
-        float bv[NS], cv[NS], red[NS];
-        b.prev(bv);
-        c.prev(cv);
+        if (j == SUB / 2 - 1 && s && m > SUB / 2) request(s - 1);
+        bv = next_b;
+        cv = next_c;
+        if (j) {
+          b.prev(next_b);
+          c.prev(next_c);
+        }
         const In in = inputs[j][lane];
         const float xv = to_f(in.x), up = to_f(in.dy);
-        float g = up, zv = 0.f, sig = 0.f;
+        float g = up, zv = 0.f, sig = 0.f, red[NS];
         if constexpr (GATED) {
           zv = to_f(in.z);
           sig = sigmoid(zv);
           g *= zv * sig;
         }
+        // (a lane past the last channel stands in for it and writes what it writes, but must not be in the sums over the channels)
+        const float u = delta[j] * xv, u_in = valid ? u : 0.f, g_in = valid ? g : 0.f;
         float y = skip * xv;
 #pragma unroll
         for (int n = 0; n < NS; n++) {
           if constexpr (GATED) y = fmaf(cv[n], h[j][n], y);
-          red[n] = h[j][n] * g;
+          G[n] = fmaf(cv[n], g, G[n]);
+          red[n] = h[j][n] * g_in;
         }
         const float sum_c = wave_sums<NS>(red, lane);
         if (j == 0) restore(before, h0);
         const float (&hp)[NS] = j ? h[j - 1] : h0;
-        const float u = delta[j] * xv;
         float du = 0.f, dd = 0.f;
 #pragma unroll
         for (int n = 0; n < NS; n++) {
-          G[n] = fmaf(cv[n], g, G[n]);
-          red[n] = G[n] * u;
+          red[n] = G[n] * u_in;
           du = fmaf(G[n], bv[n], du);
           G[n] *= ex2(delta[j] * a2[n]);
           const float r = G[n] * hp[n];
@@ -350,22 +368,18 @@ scan_grads_kernel(ScanArgs a, int blocks, int strips, GradBuffers buf) {
           dA[n] = fmaf(delta[j], r, dA[n]);
         }
         const float sum_b = wave_sums<NS>(red, lane);
-        // the lanes of an entry: one stores its dB, one its dC
-        constexpr int SHARE = WAVE / NS, HALF = SHARE / 2;
-        if (lane % HALF == 0)
-          buf.bc[((int64_t)block * a.n_tokens + t0 + t) * (2 * NS) + (lane % SHARE ? NS : 0) + lane / SHARE] = lane % SHARE ? sum_c : sum_b;
+        bc.so = (base + j) * bc.step;
+        bc.put(bc_off, lane & HALF ? sum_c : sum_b);
         dD = fmaf(g, xv, dD);
         dd = fmaf(xv, du, dd * LN2);
         float slope = sigmoid(to_f(in.dt) + bias);
         asm volatile("" : "+v"(slope));
         dd *= a.use_softplus ? slope : 1.f;
         dbias += dd;
-        dx.so = ddt.so = dz.so = t * dx.step;
-        if (valid) {
-          dx.put(off, fmaf(delta[j], du, skip * g));
-          ddt.put(off, dd);
-          if constexpr (GATED) dz.put(off, up * y * sig * (1.f + zv * (1.f - sig)));
-        }
+        dx.so = ddt.so = dz.so = (base + j) * dx.step;
+        dx.put(off, fmaf(delta[j], du, skip * g));
+        ddt.put(off, dd);
+        if constexpr (GATED) dz.put(off, up * y * sig * (1.f + zv * (1.f - sig)));
       }
     }
   }
@@ -430,7 +444,7 @@ int strips_of(int channels, int n_chunks) {
 size_t scan_bwd_workspace(int64_t n_tokens, int channels, int n_state, int n_chunks, int n_slots) {
   const size_t width = (size_t)channels * n_state * sizeof(float);
   const size_t blocks = (channels + WAVE - 1) / WAVE, strips = strips_of(channels, n_chunks);
-  return 2 * up(width * n_chunks) + up((size_t)channels * n_chunks * sizeof(float)) + up(width * n_slots) +
+  return 2 * up(width * n_chunks) + up((size_t)channels * n_chunks * sizeof(float)) + up(2 * width * n_slots) +
          up(width * fronts(n_tokens)) + up((size_t)channels * fronts(n_tokens) * sizeof(float)) +
          up(blocks * n_tokens * 2 * n_state * sizeof(float)) + up(strips * width) + up(strips * 2 * channels * sizeof(float)) + 256;
 }
@@ -443,7 +457,7 @@ hipError_t scan_bwd(const ScanArgs& a, hipStream_t st) {
   float* local = take(width * a.n_chunks);
   float* back = take(width * a.n_chunks);
   float* steps = take((size_t)a.channels * a.n_chunks * sizeof(float));
-  float* slots = take(width * a.n_slots);
+  float* slots = take(2 * width * a.n_slots);
   float* front_states = take(width * fronts(a.n_tokens));
   float* front_steps = take((size_t)a.channels * fronts(a.n_tokens) * sizeof(float));
   GradBuffers buf{local, back, front_states, front_steps, nullptr, nullptr, nullptr};
@@ -463,7 +477,7 @@ hipError_t scan_bwd(const ScanArgs& a, hipStream_t st) {
     if (hipError_t e = hipGetLastError()) return e;
     if (a.n_chunks > 0 || a.d_initial_state) {
       KernelTimer timer(TT_KERNEL_SCAN_STATES, st);
-      const unsigned walkers = (unsigned)((NS * (int64_t)a.channels + WALK_THREADS - 1) / WALK_THREADS);
+      const dim3 walkers((unsigned)((NS * (int64_t)a.channels + WALK_THREADS - 1) / WALK_THREADS), 2);
       const size_t lds = (size_t)a.n_slots * WALK_THREADS * sizeof(float);
       if (a.n_slots <= LDS_SLOTS) scan_bwd_states_kernel<true><<<walkers, WALK_THREADS, lds, st>>>(a, local, back, steps, slots);
       else scan_bwd_states_kernel<false><<<walkers, WALK_THREADS, 0, st>>>(a, local, back, steps, slots);
