@@ -695,9 +695,10 @@ tt_status tt_tree_gdn_bwd(int64_t n_tokens, int32_t hk, int32_t hv, int32_t dk, 
  * (device copies; chunk_cap may be NULL = nothing captured).  The forward takes chunks of at most
  * TT_SCAN_CHUNK_MAX tokens, the backward of at most TT_GDN_CHUNK (what lies behind them in a longer chunk
  * is not computed).
- * tt_tree_scan_join (host): the program with the chunks of one run joined as far as the forward is the
- *   faster for it with this many channels: arrays of n_chunks entries, *n_joined of them written (cap may
- *   be NULL).  The results are those of the program itself up to rounding.
+ * tt_tree_scan_program (host): the same program with every run of chunks that continue each other cut anew, into
+ *   pieces of the length that the forward (backward = 0) or backward (1) is fast with for this many channels.
+ *   *n_pieces pieces; all outputs NULL = only that number; cap may be NULL.  Results are those of the given
+ *   program up to rounding.
  *   x, dt, z, y, dy [n_tokens][channels], b, c [n_tokens][groups][n_state], dtype bf16 or fp32, token
  *   strides in elements (0 = contiguous, below 2^19); A [channels][n_state] (rates, negative), D, dt_bias [channels]
  *   or NULL (= 0), fp32; n_state 4, 8 or 16; groups divides channels, and with several groups
@@ -716,8 +717,7 @@ tt_status tt_tree_gdn_bwd(int64_t n_tokens, int32_t hk, int32_t hv, int32_t dk, 
  * Errors: TT_ERR_NULL, TT_ERR_SHAPE, TT_ERR_DTYPE, TT_ERR_ALIGN, TT_ERR_UNSUPPORTED (n_state, groups),
  *   TT_ERR_WORKSPACE; the workspace functions return 0 for an invalid descriptor.
  * ------------------------------------------------------------------------------------------ */
-#define TT_SCAN_CHUNK_MAX 1024      /* most tokens of a joined chunk                                       */
-#define TT_SCAN_MIN_WAVES 12288   /* chunks times blocks of 64 channels below which none are joined further */
+#define TT_SCAN_CHUNK_MAX 1024
 typedef struct {
   int64_t n_tokens;
   int32_t channels, n_state, groups;
@@ -729,10 +729,10 @@ typedef struct {
   int32_t n_chunks, n_slots;
   const int32_t *chunk_tok0, *chunk_len, *chunk_src, *chunk_dst, *chunk_cap;      /* device */
 } tt_scan_chunks;
-tt_status tt_tree_scan_join(int32_t n_chunks, const int32_t* chunk_tok0, const int32_t* chunk_len,
-                            const int32_t* chunk_src, const int32_t* chunk_dst, const int32_t* chunk_cap,
-                            int32_t channels, int32_t* n_joined, int32_t* tok0, int32_t* len, int32_t* src,
-                            int32_t* dst, int32_t* cap);
+tt_status tt_tree_scan_program(int32_t n_chunks, const int32_t* chunk_tok0, const int32_t* chunk_len,
+                               const int32_t* chunk_src, const int32_t* chunk_dst, const int32_t* chunk_cap,
+                               int32_t channels, int32_t backward, int32_t* n_pieces, int32_t* tok0, int32_t* len,
+                               int32_t* src, int32_t* dst, int32_t* cap);
 size_t tt_tree_scan_fwd_workspace(const tt_scan_desc* desc, int32_t n_chunks, int32_t n_slots);
 size_t tt_tree_scan_bwd_workspace(const tt_scan_desc* desc, int32_t n_chunks, int32_t n_slots);
 tt_status tt_tree_scan_fwd(const tt_scan_desc* desc, const tt_scan_chunks* chunks, const void* x, const void* dt,

@@ -152,8 +152,8 @@ def _lib() -> ctypes.CDLL:
                                         _vp, _vp, _vp, _vp, _vp, _vp, ctypes.c_int32, _vp, _vp, _vp, _vp, ctypes.c_int32, _vp, _vp, _vp, _vp,
                                         _vp, _vp, _vp, _vp, _vp, _vp, _vp, ctypes.c_size_t, _vp]
         desc, chunks = ctypes.POINTER(_ScanDesc), ctypes.POINTER(_ScanChunks)
-        lib.tt_tree_scan_join.restype = ctypes.c_int32
-        lib.tt_tree_scan_join.argtypes = [ctypes.c_int32] + [_vp] * 5 + [ctypes.c_int32, _c_i32p] + [_vp] * 5
+        lib.tt_tree_scan_program.restype = ctypes.c_int32
+        lib.tt_tree_scan_program.argtypes = [ctypes.c_int32] + [_vp] * 5 + [ctypes.c_int32, ctypes.c_int32, _c_i32p] + [_vp] * 5
         for name in ("tt_tree_scan_fwd_workspace", "tt_tree_scan_bwd_workspace"):
             getattr(lib, name).restype = ctypes.c_size_t
             getattr(lib, name).argtypes = [desc, ctypes.c_int32, ctypes.c_int32]
@@ -352,7 +352,7 @@ class GdnPlan:
     slot_cons_off: Optional[np.ndarray] = None
     slot_cons: Optional[np.ndarray] = None
     parallel: bool = True          # False: the device calls walk all chunks in sequence order (for cross-checks)
-    scan_joined: Optional[dict] = None     # (channels, device) -> tt_tree_scan_join's program on that device
+    scan_programs: Optional[dict] = None   # the scan's programs, by channels and direction, on the host and on devices
 
     @property
     def n_segments(self) -> int:
@@ -370,26 +370,31 @@ class GdnPlan:
         self.device = {n: torch.from_numpy(getattr(self, n)).to(device) for n in names}
         return self
 
-    def _scan_chunks(self, channels: Optional[int], device, captured: bool):
-        """ctypes tt_scan_chunks on `device`: the program joined for the scan's forward with this many channels, or (None) as
-        it is.  Laid out once per number of channels."""
-        if self.scan_joined is None:
-            self.scan_joined = {}
-        prog = self.scan_joined.get((channels, device))
+    def _scan_program(self, channels: int, backward: bool):
+        """tt_tree_scan_program for the scan with this many channels, [5, pieces] int32.  Laid out once per number of channels."""
+        if self.scan_programs is None:
+            self.scan_programs = {}
+        prog = self.scan_programs.get((channels, backward))
         if prog is None:
-            torch = _torch()
-            arrays = [self.chunk_tok0, self.chunk_len, self.chunk_src, self.chunk_dst, self.chunk_cap]
-            if channels is not None:
-                n = ctypes.c_int32(0)
-                out = [np.zeros(self.n_chunks, np.int32) for _ in range(5)]
-                _check(_lib().tt_tree_scan_join(self.n_chunks, *(_hp(a) for a in arrays), channels, ctypes.byref(n), *(_hp(a) for a in out)))
-                arrays = [a[:n.value] for a in out]
-            packed = torch.from_numpy(np.stack(arrays)).to(device)
-            rows = [packed[i].data_ptr() for i in range(5)]
-            n = packed.shape[1]
-            prog = self.scan_joined[(channels, device)] = (packed, _ScanChunks(n, self.n_slots, *rows[:4], None),
-                                                           _ScanChunks(n, self.n_slots, *rows))
-        return prog[2 if captured else 1]
+            f, n = _lib().tt_tree_scan_program, ctypes.c_int32(0)
+            given = [_hp(a) for a in (self.chunk_tok0, self.chunk_len, self.chunk_src, self.chunk_dst, self.chunk_cap)]
+            _check(f(self.n_chunks, *given, channels, int(backward), ctypes.byref(n), *[None] * 5))
+            prog = np.zeros((5, n.value), np.int32)
+            _check(f(self.n_chunks, *given, channels, int(backward), ctypes.byref(n), *(_hp(a) for a in prog)))
+            self.scan_programs[(channels, backward)] = prog
+        return prog
+
+    def _scan_chunks(self, channels: int, backward: bool, device, captured: bool):
+        """ctypes tt_scan_chunks of that program on `device`."""
+        prog = self._scan_program(channels, backward)
+        key = (channels, backward, device)
+        on_device = self.scan_programs.get(key)
+        if on_device is None:
+            packed = _torch().from_numpy(prog).to(device)
+            rows, n = [packed[i].data_ptr() for i in range(5)], prog.shape[1]
+            on_device = self.scan_programs[key] = (packed, _ScanChunks(n, self.n_slots, *rows[:4], None),
+                                                   _ScanChunks(n, self.n_slots, *rows))
+        return on_device[2 if captured else 1]
 
     def _schedule(self):
         """ctypes tt_gdn_schedule for the device calls, or None (sequential walk)."""
@@ -1169,7 +1174,7 @@ def tree_scan_fwd(x, dt, A, B, C, plan: GdnPlan, *, D=None, z=None, dt_bias=None
     with _launch_on(x, dt, A, B, C, D, z, dt_bias, initial_state, out, workspace):
         dev = x.device
         captured = return_states and plan.n_capture > 0
-        chunks = plan._scan_chunks(ch, dev, captured)
+        chunks = plan._scan_chunks(ch, False, dev, captured)
         if out is None:
             out = torch.empty((n, ch), dtype=x.dtype, device=dev)
         states = torch.empty((plan.n_capture, ch, m), dtype=torch.float32, device=dev) if return_states else None
@@ -1186,9 +1191,8 @@ def tree_scan_workspace(x, A, B, plan: GdnPlan, backward: bool = False) -> int:
     """Bytes of workspace of tree_scan_fwd or tree_scan_bwd for tensors of these shapes."""
     torch = _torch()
     desc = _ScanDesc(x.shape[0], x.shape[1], A.shape[1], B.shape[1], DTYPE_BF16 if x.dtype == torch.bfloat16 else DTYPE_FP32, 1)
-    if backward:
-        return int(_lib().tt_tree_scan_bwd_workspace(ctypes.byref(desc), plan.n_chunks, plan.n_slots))
-    return int(_lib().tt_tree_scan_fwd_workspace(ctypes.byref(desc), plan.n_chunks, plan.n_slots))
+    f = _lib().tt_tree_scan_bwd_workspace if backward else _lib().tt_tree_scan_fwd_workspace
+    return int(f(ctypes.byref(desc), plan._scan_program(x.shape[1], backward).shape[1], plan.n_slots))
 
 
 def tree_scan_bwd(x, dt, A, B, C, d_y, plan: GdnPlan, *, D=None, z=None, dt_bias=None, softplus: bool = True, initial_state=None,
@@ -1208,7 +1212,7 @@ def tree_scan_bwd(x, dt, A, B, C, d_y, plan: GdnPlan, *, D=None, z=None, dt_bias
     with _launch_on(x, dt, A, B, C, D, z, dt_bias, initial_state, d_y, d_state_out, workspace):
         dev = x.device
         captured = d_state_out is not None and plan.n_capture > 0
-        chunks = plan._scan_chunks(None, dev, captured)
+        chunks = plan._scan_chunks(ch, True, dev, captured)
         like = lambda t: None if t is None else torch.empty(t.shape, dtype=t.dtype, device=dev)      # noqa: E731
         grads = ScanGrads(like(x), like(x), like(A), like(B), like(C), like(D), like(z), like(dt_bias), like(A) if want_d_initial_state else None)
         need = int(_lib().tt_tree_scan_bwd_workspace(ctypes.byref(desc), chunks.n_chunks, chunks.n_slots))

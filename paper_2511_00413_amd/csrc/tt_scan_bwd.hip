@@ -433,10 +433,11 @@ scan_sums_kernel(ScanArgs a, int blocks, int strips, GradBuffers buf, int64_t bc
 size_t up(size_t v) { return (v + 255) & ~(size_t)255; }
 
 // Strips of chunks that one wave per channel block takes one after the other, keeping dA in registers: as many as give the chip
-// 4096 waves, twice what it holds at a time.
+// 6144 waves, three times what it holds at a time (2048 / 4096 / 6144 / 8192 waves and one chunk each, with the sums over the strips,
+// 16406 tokens of 4096 channels: 1031 / 1021 / 1002 / 1016 / 1009 us).
 int strips_of(int channels, int n_chunks) {
   const int blocks = (channels + WAVE - 1) / WAVE;
-  return std::max(1, std::min(n_chunks, (4096 + blocks - 1) / blocks));
+  return std::max(1, std::min(n_chunks, (6144 + blocks - 1) / blocks));
 }
 
 }  // namespace

@@ -1,9 +1,12 @@
-"""tt_tree_scan_join (host): the joined chunk program walks the same tree."""
+"""tt_tree_scan_program (host): the program cut anew walks the same tree."""
+import ctypes
+
 import numpy as np
 import pytest
 
 import paper_2511_00413_amd as T
 import workloads as W
+from paper_2511_00413_amd import binding as B
 
 
 def ends(tok0, length, src, dst, cap, n_slots):
@@ -21,39 +24,38 @@ def ends(tok0, length, src, dst, cap, n_slots):
     return pred, slot, caps
 
 
+@pytest.mark.parametrize("backward", [False, True])
 @pytest.mark.parametrize("channels", [8, 256, 4096, 65536])
 @pytest.mark.parametrize("seed,lo,hi", [(1, 0, 40), (2, 50, 900), (3, 1, 3000)])
-def test_joined_program(seed, lo, hi, channels):
+def test_program(seed, lo, hi, channels, backward):
     tree = W.random_tree(seed, n_nodes=25, lo=lo, hi=hi, n_roots=2)
     cuts = [i for i in range(25) if tree.seg_len[i] > 0][3::7]
     plan = T.tree_gdn_plan(tree.parent, tree.seg_len, cuts)
-    from paper_2511_00413_amd import binding as B
-    import ctypes
+    out = plan._scan_program(channels, backward).tolist()
     arrays = [plan.chunk_tok0, plan.chunk_len, plan.chunk_src, plan.chunk_dst, plan.chunk_cap]
-    out, n = [np.zeros(plan.n_chunks, np.int32) for _ in range(5)], ctypes.c_int32(0)
-    B._check(B._lib().tt_tree_scan_join(plan.n_chunks, *(B._hp(a) for a in arrays), channels, ctypes.byref(n), *(B._hp(a) for a in out)))
-    out = [a[:n.value].tolist() for a in out]
     assert ends(*out, plan.n_slots) == ends(*(a.tolist() for a in arrays), plan.n_slots)
-    assert max(out[1]) <= 1024 and n.value <= plan.n_chunks
-    waves = -(-channels // 64)
-    assert max(out[1]) <= 64 or n.value * waves >= 12288
+    assert max(out[1]) <= (64 if backward else 1024) and min(out[1]) >= 1
+    waves = len(out[0]) * -(-channels // 64)
+    assert max(out[1]) <= 16 or waves >= (12288 if max(out[1]) > 64 else 4096)
 
 
-def test_refusals():
-    from paper_2511_00413_amd import binding as B
-    import ctypes
+def test_empty_and_refusals():
     n, a = ctypes.c_int32(0), [np.array(v, np.int32) for v in ([0, 64], [64, 64], [-1, -2], [-1, -1], [-1, -1])]
-    out = [np.zeros(2, np.int32) for _ in range(5)]
-    f = B._lib().tt_tree_scan_join
+    out = [np.zeros(8, np.int32) for _ in range(5)]
+    f = B._lib().tt_tree_scan_program
     p = lambda v: [B._hp(x) for x in v]                                       # noqa: E731
-    assert f(2, *p(a), 64, ctypes.byref(n), *p(out)) == 0 and n.value == 2
-    assert f(2, *p(a), 0, ctypes.byref(n), *p(out)) == -2
-    assert f(-1, *p(a), 64, ctypes.byref(n), *p(out)) == -2
-    assert f(2, *p(a[:3]), None, None, 64, ctypes.byref(n), *p(out)) == -1
+    assert f(2, *p(a), 64, 0, ctypes.byref(n), *p(out)) == 0 and n.value == 8 and out[1].tolist() == [16] * 8
+    assert f(2, *p(a), 64, 0, ctypes.byref(n), *[None] * 5) == 0 and n.value == 8
+    assert f(2, *p(a), 64, 0, ctypes.byref(n), *p(out[:4]), None) == 0
+    assert f(2, *p(a), 0, 0, ctypes.byref(n), *p(out)) == -2
+    assert f(-1, *p(a), 64, 0, ctypes.byref(n), *p(out)) == -2
+    assert f(2, *p(a[:3]), None, None, 64, 0, ctypes.byref(n), *p(out)) == -1
+    assert f(2, *p(a), 64, 0, ctypes.byref(n), None, *p(out[1:])) == -1
+    assert f(2, *p(a), 64, 0, None, *p(out)) == -1
     bad = [x.copy() for x in a]
     bad[0][1] = 63
-    assert f(2, *p(bad), 64, ctypes.byref(n), *p(out)) == -3
+    assert f(2, *p(bad), 64, 0, ctypes.byref(n), *p(out)) == -3
     bad = [x.copy() for x in a]
     bad[1][0] = 0
-    assert f(2, *p(bad), 64, ctypes.byref(n), *p(out)) == -3
-    assert f(0, None, None, None, None, None, 64, ctypes.byref(n), None, None, None, None, None) == 0 and n.value == 0
+    assert f(2, *p(bad), 64, 0, ctypes.byref(n), *p(out)) == -3
+    assert f(0, None, None, None, None, None, 64, 1, ctypes.byref(n), None, None, None, None, None) == 0 and n.value == 0
