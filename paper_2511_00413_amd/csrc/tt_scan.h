@@ -167,6 +167,31 @@ struct Slots {
   __device__ __forceinline__ float& operator[](int s) const { return p[s * step]; }
 };
 
+// WALK rows of [n_chunks][width] and [n_chunks][channels] arrays from row u0 on; rows past the end are the last one again.
+struct WalkRows {
+  int n_chunks, channels;
+  int64_t width;
+  uint32_t at, c;                               // the lane's offsets in bytes
+  __device__ __forceinline__ WalkRows(const ScanArgs& a, int64_t w, int64_t at_, int c_)
+      : n_chunks(a.n_chunks), channels(a.channels), width(w), at((uint32_t)at_ * 4u), c((uint32_t)c_ * 4u) {}
+  __device__ __forceinline__ void load(const float* values, const float* steps, int u0, float (&h)[WALK], float (&d)[WALK]) const {
+    const int first = min(u0, n_chunks - 1);
+    Feed<float> x(values, width, first), y(steps, channels, first);
+#pragma unroll
+    for (int j = 0; j < WALK; j++) {
+      const bool more = u0 + j < n_chunks - 1;
+      h[j] = x.next(at, more);
+      d[j] = y.next(c, more);
+    }
+  }
+  __device__ __forceinline__ void store(float* values, int u0, const float (&h)[WALK]) const {
+    Feed<float> x(values, width, u0);
+#pragma unroll
+    for (int j = 0; j < WALK; j++, x.so += x.step)
+      if (u0 + j < n_chunks) x.put(at, h[j]);
+  }
+};
+
 // Down the tree: replaces add[chunk] by the state entering the chunk.  leave(cap, state) sees the captured states.
 // (Lanes past the last entry stand in for it: they write what it writes.)
 template <bool LDS, typename Leave>
@@ -174,14 +199,8 @@ __device__ __forceinline__ void walk_down(const ScanArgs& a, float* local, const
                                           float a2, float first, const Slots<LDS>& slots, bool with_cap, Leave leave) {
   Program prog;
   float s = first, add[2][WALK], len[2][WALK];
-  auto request = [&](int u0, float (&h)[WALK], float (&d)[WALK]) {
-#pragma unroll
-    for (int j = 0; j < WALK; j++) {
-      const int64_t u = min(u0 + j, a.n_chunks - 1);
-      h[j] = local[u * width + at];
-      d[j] = steps[u * a.channels + c];
-    }
-  };
+  const WalkRows rows(a, width, at, c);
+  auto request = [&](int u0, float (&h)[WALK], float (&d)[WALK]) { rows.load(local, steps, u0, h, d); };
   auto walk = [&](int u0, const float (&h)[WALK], const float (&d)[WALK]) {
     float entering[WALK];
 #pragma unroll
@@ -197,9 +216,7 @@ __device__ __forceinline__ void walk_down(const ScanArgs& a, float* local, const
         if (cap >= 0) leave(cap, s);
       }
     }
-#pragma unroll
-    for (int j = 0; j < WALK; j++)
-      if (u0 + j < a.n_chunks) local[(int64_t)(u0 + j) * width + at] = entering[j];
+    rows.store(local, u0, entering);
   };
   request(0, add[0], len[0]);
   for (int u0 = 0; u0 < a.n_chunks; u0 += 2 * WALK) {

@@ -126,14 +126,8 @@ scan_bwd_states_kernel(ScanArgs a, float* local, float* back, const float* __res
   Program prog;
   float sent = 0.f, d_first = 0.f, add[2][WALK], len[2][WALK];
   int nxt_src = -1;                                                            // of the chunk behind
-  auto request = [&](int top, float (&r)[WALK], float (&d)[WALK]) {
-#pragma unroll
-    for (int j = 0; j < WALK; j++) {
-      const int64_t u = max(min(top - j, a.n_chunks - 1), 0);
-      r[j] = back[u * width + at];
-      d[j] = steps[u * a.channels + c];
-    }
-  };
+  const WalkRows rows(a, width, at, c);
+  auto request = [&](int top, float (&r)[WALK], float (&d)[WALK]) { rows.load(back, steps, top - WALK + 1, r, d); };
   auto walk = [&](int top, const float (&r)[WALK], const float (&d)[WALK]) {
     float leaving[WALK];
 #pragma unroll
@@ -145,16 +139,14 @@ scan_bwd_states_kernel(ScanArgs a, float* local, float* back, const float* __res
         bool used = nxt_src == -2;
         if (dst >= 0) { g += slots[dst]; used = true; }
         if (cap >= 0) { g += a.d_state_out[cap * width + state_at]; used = true; }
-        leaving[j] = g;
-        sent = used ? fmaf(ex2(d[j] * a2), g, r[j]) : r[j];                    // (steps are not there where no state is used)
+        leaving[WALK - 1 - j] = g;
+        sent = used ? fmaf(ex2(d[WALK - 1 - j] * a2), g, r[WALK - 1 - j]) : r[WALK - 1 - j];      // (steps are not there where no state is used)
         if (src == -1) d_first += sent;
         else if (src >= 0) slots[src] += sent;
         nxt_src = src;
       }
     }
-#pragma unroll
-    for (int j = 0; j < WALK; j++)
-      if (top - j >= 0 && top - j < a.n_chunks) back[(int64_t)(top - j) * width + at] = leaving[j];
+    rows.store(back, top - WALK + 1, leaving);
   };
   const int last = (a.n_chunks + 2 * WALK - 1) / (2 * WALK) * (2 * WALK) - 1;   // whole rounds: 64 entries at a time line up
   request(last, add[0], len[0]);
