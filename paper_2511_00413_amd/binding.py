@@ -1,8 +1,8 @@
 """ctypes binding of libtreetrain.so.  Argument marshalling only."""
 from __future__ import annotations
 
-import contextlib
 import ctypes
+import functools
 import os
 from dataclasses import dataclass
 from typing import NamedTuple, Optional
@@ -597,36 +597,46 @@ def _workspace(desc, backward, workspace, device):
 
 def _check_tensor(t, name, shape, dtype):
     """A contiguous tensor of exactly this shape and dtype."""
-    if tuple(t.shape) != tuple(shape) or t.dtype != dtype or not t.is_contiguous():
-        raise ValueError(f"{name} must be a contiguous {dtype} tensor of shape {tuple(shape)}")
+    if t.shape != shape or t.dtype is not dtype or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous {dtype} tensor of shape {shape}")
 
 
 def _check_rows(t, name, shape, dtypes):
     """Rows of contiguous elements with a free stride between them (one of the dtypes); returns that stride in elements."""
-    if tuple(t.shape) != tuple(shape) or t.dtype not in dtypes:
-        raise ValueError(f"{name} must be {tuple(shape)} of {' / '.join(str(d) for d in dtypes)}")
+    if t.shape != shape or t.dtype not in dtypes:
+        raise ValueError(f"{name} must be {shape} of {' / '.join(str(d) for d in dtypes)}")
+    step = t.stride()
     row = 1
-    for size, step in zip(t.shape[:0:-1], t.stride()[:0:-1]):
-        if size > 1 and step != row:
+    for i in range(len(shape) - 1, 0, -1):
+        if shape[i] > 1 and step[i] != row:
             raise ValueError(f"the rows of {name} must be contiguous (only the stride between them is free)")
-        row *= size
-    if t.shape[0] <= 1:
+        row *= shape[i]
+    if shape[0] <= 1:
         return row
-    if t.stride(0) < row:
+    if step[0] < row:
         raise ValueError(f"the rows of {name} overlap")
-    return t.stride(0)
+    return step[0]
 
 
-def _launch_on(first, *others):
-    """Context in which a call on these tensors is made: their device, which must be one and the same GPU, is current."""
-    torch = _torch()
-    dev = first.device
-    if dev.type != "cuda":
+def _enter_device(*tensors):
+    """Makes the tensors' device, which must be one and the same GPU, the current one.  Returns what _leave_device wants."""
+    dev = tensors[0].get_device()
+    for t in tensors:
+        if t is not None and t.get_device() != dev:
+            raise ValueError(f"tensors on {tensors[0].device} and {t.device} in one call")
+    if dev < 0:
         raise ValueError("the tensors must be on the GPU")
-    for t in others:
-        if t is not None and t.device != dev:
-            raise ValueError(f"tensors on {dev} and {t.device} in one call")
-    return contextlib.nullcontext() if dev.index == torch.cuda.current_device() else torch.cuda.device(dev)
+    cuda = _torch().cuda
+    before = cuda.current_device()
+    if before == dev:
+        return None
+    cuda.set_device(dev)
+    return before
+
+
+def _leave_device(before):
+    if before is not None:
+        _torch().cuda.set_device(before)
 
 
 def tree_attn_fwd(q, k, v, kend, kt_min, kt_max, *, k_prefix=None, v_prefix=None, scale=None,
@@ -717,8 +727,8 @@ def tree_rope(x, tok_pos, *, theta_base: float = 1.0e6, inverse: bool = False, o
     return out
 
 
-def _pair_axis(sections, n_axes: int, half: int, interleaved: bool) -> bytes:
-    sections = tuple(int(s) for s in sections)
+@functools.lru_cache(maxsize=64)
+def _pair_axis(sections: tuple, n_axes: int, half: int, interleaved: bool) -> bytes:
     if len(sections) != n_axes or min(sections) < 0 or sum(sections) != half:
         raise ValueError(f"sections must hold one non-negative count per axis ({n_axes}), {half} pairs together")
     if not interleaved:
@@ -743,16 +753,19 @@ def tree_rope_axes(x, axis_pos, sections, *, interleaved: bool = False, theta_ba
         raise ValueError("axis_pos must have 1 to 4 axes")
     if d % 2:
         raise ValueError("d must be even")
-    pair_axis = _pair_axis(sections, n_axes, d // 2, interleaved)
+    pair_axis = _pair_axis(tuple(sections), n_axes, d // 2, bool(interleaved))
     out_stride = h * d
     if out is not None:
         out_stride = _check_rows(out, "out", (n, h, d), (x.dtype,))
-    with _launch_on(x, axis_pos, out):
+    before = _enter_device(x, axis_pos, out)
+    try:
         if out is None:
             out = torch.empty((n, h, d), dtype=x.dtype, device=x.device)
         _check(_lib().tt_tree_rope_axes(n, h, d, DTYPE_BF16 if x.dtype == torch.bfloat16 else DTYPE_FP32, _dp(x), stride, n_axes,
                                         _dp(axis_pos), pair_axis, float(theta_base), 1 if inverse else 0, _dp(out), out_stride,
                                         _stream_ptr(stream)))
+    finally:
+        _leave_device(before)
     return out
 
 
@@ -814,7 +827,8 @@ def tree_logprob_entropy(logits, target, *, top_k: int = 0, logp=None, entropy=N
         _check_tensor(top_index, "top_index", (n, top_k), torch.int32)
     if top_logp is not None:
         _check_tensor(top_logp, "top_logp", (n, top_k), torch.float32)
-    with _launch_on(logits, target, logp, entropy, lse, top_index, top_logp, workspace):
+    before = _enter_device(logits, target, logp, entropy, lse, top_index, top_logp, workspace)
+    try:
         dev = logits.device
         new = lambda *shape, dtype=torch.float32: torch.empty(shape, dtype=dtype, device=dev)      # noqa: E731
         logp, entropy, lse = (new(n) if t is None else t for t in (logp, entropy, lse))
@@ -826,6 +840,8 @@ def tree_logprob_entropy(logits, target, *, top_k: int = 0, logp=None, entropy=N
         _check(_lib().tt_tree_logprob_entropy(n, vocab, code, _dp(logits), stride, _dp(target), top_k, _dp(logp), _dp(entropy),
                                               _dp(lse), _dp(top_index), _dp(top_logp), _dp(workspace),
                                               workspace.numel() * workspace.element_size(), _stream_ptr(stream)))
+    finally:
+        _leave_device(before)
     return logp, entropy, lse, top_index, top_logp
 
 
@@ -845,11 +861,14 @@ def tree_logprob_entropy_bwd(logits, target, lse, entropy, d_logp=None, d_entrop
     out_stride = vocab
     if out is not None:
         out_stride = _check_rows(out, "out", (n, vocab), (logits.dtype,))
-    with _launch_on(logits, target, lse, entropy, d_logp, d_entropy, out):
+    before = _enter_device(logits, target, lse, entropy, d_logp, d_entropy, out)
+    try:
         if out is None:
             out = torch.empty((n, vocab), dtype=logits.dtype, device=logits.device)
         _check(_lib().tt_tree_logprob_entropy_bwd(n, vocab, code, _dp(logits), stride, _dp(target), _dp(lse), _dp(entropy),
                                                   _dp(d_logp), _dp(d_entropy), _dp(out), out_stride, _stream_ptr(stream)))
+    finally:
+        _leave_device(before)
     return out
 
 
@@ -1171,7 +1190,8 @@ def tree_scan_fwd(x, dt, A, B, C, plan: GdnPlan, *, D=None, z=None, dt_bias=None
     if initial_state is not None:
         _check_tensor(initial_state, "initial_state", (ch, m), torch.float32)
     desc.y_stride_tok = _check_rows(out, "out", (n, ch), (x.dtype,)) if out is not None else ch
-    with _launch_on(x, dt, A, B, C, D, z, dt_bias, initial_state, out, workspace):
+    before = _enter_device(x, dt, A, B, C, D, z, dt_bias, initial_state, out, workspace)
+    try:
         dev = x.device
         captured = return_states and plan.n_capture > 0
         chunks = plan._scan_chunks(ch, False, dev, captured)
@@ -1184,6 +1204,8 @@ def tree_scan_fwd(x, dt, A, B, C, plan: GdnPlan, *, D=None, z=None, dt_bias=None
         _check(_lib().tt_tree_scan_fwd(ctypes.byref(desc), ctypes.byref(chunks), _dp(x), _dp(dt), _dp(A), _dp(B), _dp(C), _dp(D), _dp(z),
                                        _dp(dt_bias), _dp(initial_state), _dp(states) if captured else None, _dp(out), _dp(workspace),
                                        workspace.numel() * workspace.element_size(), _stream_ptr(stream)))
+    finally:
+        _leave_device(before)
     return (out, states) if return_states else out
 
 
@@ -1209,7 +1231,8 @@ def tree_scan_bwd(x, dt, A, B, C, d_y, plan: GdnPlan, *, D=None, z=None, dt_bias
     if d_state_out is not None:
         _check_tensor(d_state_out, "d_state_out", (plan.n_capture, ch, m), torch.float32)
     desc.y_stride_tok = _check_rows(d_y, "d_y", (n, ch), (x.dtype,))
-    with _launch_on(x, dt, A, B, C, D, z, dt_bias, initial_state, d_y, d_state_out, workspace):
+    before = _enter_device(x, dt, A, B, C, D, z, dt_bias, initial_state, d_y, d_state_out, workspace)
+    try:
         dev = x.device
         captured = d_state_out is not None and plan.n_capture > 0
         chunks = plan._scan_chunks(ch, True, dev, captured)
@@ -1222,6 +1245,8 @@ def tree_scan_bwd(x, dt, A, B, C, d_y, plan: GdnPlan, *, D=None, z=None, dt_bias
                                        _dp(dt_bias), _dp(initial_state), _dp(d_y), _dp(d_state_out) if captured else None,
                                        *(_dp(g) for g in grads), _dp(workspace), workspace.numel() * workspace.element_size(),
                                        _stream_ptr(stream)))
+    finally:
+        _leave_device(before)
     return grads
 
 
@@ -1241,13 +1266,16 @@ def tree_scan_step(x, dt, A, B, C, state, *, index=None, D=None, z=None, dt_bias
     if state_out is not None:
         _check_tensor(state_out, "state_out", (slots if state_out is state else n, ch, m), torch.float32)
     desc.y_stride_tok = _check_rows(out, "out", (n, ch), (x.dtype,)) if out is not None else ch
-    with _launch_on(x, dt, A, B, C, D, z, dt_bias, state, index, state_out, out):
+    before = _enter_device(x, dt, A, B, C, D, z, dt_bias, state, index, state_out, out)
+    try:
         if out is None:
             out = torch.empty((n, ch), dtype=x.dtype, device=x.device)
         if state_out is None:
             state_out = torch.empty((n, ch, m), dtype=torch.float32, device=x.device)
         _check(_lib().tt_tree_scan_step(ctypes.byref(desc), _dp(x), _dp(dt), _dp(A), _dp(B), _dp(C), _dp(D), _dp(z), _dp(dt_bias), slots,
                                         _dp(state), _dp(index), _dp(state_out), _dp(out), _stream_ptr(stream)))
+    finally:
+        _leave_device(before)
     return out, state_out
 
 
@@ -1271,7 +1299,8 @@ def tree_conv_step(x, state, weight, bias=None, *, index=None, silu: bool = True
     if state_out is not None:
         _check_tensor(state_out, "state_out", (slots if state_out is state else n, k - 1, c), x.dtype)
     ys = _check_rows(out, "out", (n, c), (x.dtype,)) if out is not None else c
-    with _launch_on(x, state, weight, bias, index, state_out, out):
+    before = _enter_device(x, state, weight, bias, index, state_out, out)
+    try:
         if out is None:
             out = torch.empty((n, c), dtype=x.dtype, device=x.device)
         if state_out is None:
@@ -1279,4 +1308,6 @@ def tree_conv_step(x, state, weight, bias=None, *, index=None, silu: bool = True
         _check(_lib().tt_tree_conv_step(n, c, k, DTYPE_BF16 if x.dtype == torch.bfloat16 else DTYPE_FP32, 1 if silu else 0, _dp(x), xs,
                                         _dp(weight), _dp(bias), slots, _dp(state), _dp(index), _dp(state_out), _dp(out), ys,
                                         _stream_ptr(stream)))
+    finally:
+        _leave_device(before)
     return out, state_out

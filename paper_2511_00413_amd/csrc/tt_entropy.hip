@@ -55,13 +55,6 @@ __device__ __forceinline__ void add(Stat& st, float z) {
   st.s += e;
   st.u = fmaf(e, fmaxf(d, FAR), st.u);
 }
-__device__ __forceinline__ Stat merge(Stat a, Stat b) {
-  const float m = fmaxf(a.m, b.m);
-  raise(a, m);
-  raise(b, m);
-  return {m, a.s + b.s, a.u + b.u};
-}
-
 template <typename T> struct Row;
 template <> struct Row<__hip_bfloat16> {
   static constexpr int EPV = 8;
@@ -103,12 +96,25 @@ __device__ __forceinline__ float value_of(uint32_t k) { return __uint_as_float(k
 typedef unsigned long long Key;           // never 0
 __device__ __forceinline__ Key key_of(float z, int index) { return (Key)order_of(z) << 32 | (uint32_t)~index; }
 
-// maximum over the lane's group of eight
-__device__ __forceinline__ float max8(float v) {
-  v = fmaxf(v, __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(v), 0xb1, 0xf, 0xf, true)));      // quad_perm [1,0,3,2]
-  v = fmaxf(v, __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(v), 0x4e, 0xf, 0xf, true)));      // quad_perm [2,3,0,1]
-  v = fmaxf(v, __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(v), 0x141, 0xf, 0xf, true)));     // row_half_mirror
-  return v;
+// lane ^ 1, ^ 2, mirrored in eight, ^ 8 (in sixteen)
+template <int CTRL>
+__device__ __forceinline__ float dpp(float v) { return __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(v), CTRL, 0xf, 0xf, true)); }
+constexpr int XOR1 = 0xb1, XOR2 = 0x4e, HALF_MIRROR = 0x141, ROR8 = 0x128;
+__device__ __forceinline__ float max8(float v) {                 // over the lane's group of eight
+  v = fmaxf(v, dpp<XOR1>(v));
+  v = fmaxf(v, dpp<XOR2>(v));
+  return fmaxf(v, dpp<HALF_MIRROR>(v));
+}
+template <typename Op>
+__device__ __forceinline__ float wave_all(float v, Op op) {       // over the wave
+  v = op(v, dpp<XOR1>(v));
+  v = op(v, dpp<XOR2>(v));
+  v = op(v, dpp<HALF_MIRROR>(v));
+  v = op(v, dpp<ROR8>(v));
+  const auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  v = op(__uint_as_float(a[0]), __uint_as_float(a[1]));
+  const auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return op(__uint_as_float(b[0]), __uint_as_float(b[1]));
 }
 
 struct Shared {
@@ -120,6 +126,24 @@ struct Shared {
   Key last;
   alignas(16) Key list[LIST];
 };
+
+// The workgroup's sums from the threads': raised to the wave's maximum and added, then the same for the waves.
+__device__ Stat join(Shared& sh, Stat st) {
+  raise(st, wave_all(st.m, [](float a, float b) { return fmaxf(a, b); }));
+  st.s = wave_all(st.s, [](float a, float b) { return a + b; });
+  st.u = wave_all(st.u, [](float a, float b) { return a + b; });
+  if ((threadIdx.x & 63) == 0) sh.part[threadIdx.x >> 6] = st;
+  __syncthreads();
+  Stat all = {sh.part[0].m, 0.f, 0.f};
+  for (int w = 1; w < WAVES; w++) all.m = fmaxf(all.m, sh.part[w].m);
+  for (int w = 0; w < WAVES; w++) {
+    Stat p = sh.part[w];
+    raise(p, all.m);
+    all.s += p.s;
+    all.u += p.u;
+  }
+  return all;
+}
 
 // Bound from the threads' largest entries (order_of; 0 = none): the largest multiple T of 2^16 that at least k of them reach.
 // Found bit by bit by the first wave; the lower halves are left out, which keeps T a lower bound (and loses nothing in bf16).
@@ -239,32 +263,34 @@ entropy_rows_kernel(int64_t row0, int vocab, const T* __restrict__ logits, int64
     for (int e = 0; e < EPV; e++) add(st, z[e]);
   };
   if (first) for (int e = t; e < head; e += THREADS) single(e);
-  // whole rounds of 256 vectors, four in flight; the last, ragged round is taken by all lanes (those past the end stand in with
-  // -inf), so that the joins of eight lanes always have eight
-  int i = v0 + t;
-  const int full = v0 + (v1 - v0) / THREADS * THREADS;
-  for (; i + 3 * THREADS < full; i += 4 * THREADS) {
+  // Rounds of 256 vectors, four in flight.  Of the last four, those past the end are left out, and in the ragged one all lanes take
+  // part (those past the end stand in with -inf), so that the joins of eight lanes always have eight.
+  const int rounds = (v1 - v0 + THREADS - 1) / THREADS;
+  int r4 = 0;
+  for (; r4 + 4 < rounds; r4 += 4) {
+    const int i = v0 + r4 * THREADS + t;
     const u32x4 a = __builtin_nontemporal_load(vp + i);
     const u32x4 b = __builtin_nontemporal_load(vp + i + THREADS);
     const u32x4 c = __builtin_nontemporal_load(vp + i + 2 * THREADS);
     const u32x4 d = __builtin_nontemporal_load(vp + i + 3 * THREADS);
     vec(a, i); vec(b, i + THREADS); vec(c, i + 2 * THREADS); vec(d, i + 3 * THREADS);
   }
-  for (; i < full; i += THREADS) vec(__builtin_nontemporal_load(vp + i), i);
-  if (full < v1) {
+  if (r4 < rounds) {
     const uint32_t none = sizeof(T) == 2 ? 0xff80ff80u : 0xff800000u;      // -inf
-    u32x4 v = {none, none, none, none};
-    if (i < v1) v = __builtin_nontemporal_load(vp + i);
-    vec(v, i);
+    u32x4 v[4];
+#pragma unroll
+    for (int j = 0; j < 4; j++) {
+      v[j] = u32x4{none, none, none, none};
+      const int i = v0 + (r4 + j) * THREADS + t;
+      if (i < v1) v[j] = __builtin_nontemporal_load(vp + i);
+    }
+#pragma unroll
+    for (int j = 0; j < 4; j++)
+      if (r4 + j < rounds) vec(v[j], v0 + (r4 + j) * THREADS + t);
   }
   if (last) for (int e = tail0 + t; e < vocab; e += THREADS) single(e);
 
-  Stat all = st;
-  for (int o = 32; o > 0; o >>= 1) all = merge(all, {__shfl_xor(all.m, o), __shfl_xor(all.s, o), __shfl_xor(all.u, o)});
-  if ((t & 63) == 0) sh.part[t >> 6] = all;
-  __syncthreads();
-  all = sh.part[0];
-  for (int w = 1; w < WAVES; w++) all = merge(all, sh.part[w]);
+  const Stat all = join(sh, st);
   const float ln_s = LN2 * log2f(all.s);
   if (t == 0) {
     if (parts == 1) {
@@ -336,13 +362,16 @@ entropy_join_kernel(int64_t row0, int vocab, const T* __restrict__ logits, int64
   __shared__ Shared sh;
   const int64_t r = row0 + blockIdx.x;
   const int t = threadIdx.x;
-  Stat all = {LOWEST, 0.f, 0.f};
-  for (int p = t; p < parts; p += THREADS) all = merge(all, partial[r * parts + p].st);
-  for (int o = 32; o > 0; o >>= 1) all = merge(all, {__shfl_xor(all.m, o), __shfl_xor(all.s, o), __shfl_xor(all.u, o)});
-  if ((t & 63) == 0) sh.part[t >> 6] = all;
-  __syncthreads();
-  all = sh.part[0];
-  for (int w = 1; w < WAVES; w++) all = merge(all, sh.part[w]);
+  Stat st = {LOWEST, 0.f, 0.f};
+  for (int p = t; p < parts; p += THREADS) {
+    Stat q = partial[r * parts + p].st;
+    const float m = fmaxf(st.m, q.m);
+    raise(st, m);
+    raise(q, m);
+    st.s += q.s;
+    st.u += q.u;
+  }
+  const Stat all = join(sh, st);
   const float ln_s = LN2 * log2f(all.s);
   if (t == 0) {
     const int y = target[r];
