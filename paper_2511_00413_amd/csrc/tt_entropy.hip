@@ -1,9 +1,10 @@
 // Log-probability of given tokens with the entropy and the most probable alternatives, and the gradient of the first two.
 //
-// Per row of logits z:  m = max z,  s = sum e^(z - m),  u = sum e^(z - m) (z - m);
-//   lse = m + ln s,  logp = (z_y - m) - ln s,  entropy = -sum p ln p = ln s - u / s,
-// all three sums in one pass over the row: when the running maximum moves from m to m', s becomes s f and u becomes
-// f (u + s (m - m')) with f = e^(m - m').  Gradient of d_logp logp + d_entropy entropy:
+// Per row of logits z, in powers of two (x = z log2 e) against a whole number r just above the maximum of x:
+//   s = sum 2^(x - r),  u = sum 2^(x - r) (x - r);
+//   lse = ln 2 (r + log2 s),  logp = ln 2 ((x_y - r) - log2 s),  entropy = -sum p ln p = ln 2 (log2 s - u / s),
+// all in one pass over the row: when r becomes r', s becomes s f and u becomes f (u + s (r - r')), f = 2^(r - r').  r being whole, x - r
+// is one fused multiply-add with a single rounding, and the differences lose nothing.  Gradient of d_logp logp + d_entropy entropy:
 //   dz_v = d_logp ([v = y] - p_v) - d_entropy p_v (ln p_v + entropy).
 //
 // Top alternatives without a second pass: in the same pass the maximum of every block of eight 16-byte vectors goes to LDS.
@@ -27,7 +28,6 @@ constexpr int THREADS = 256;
 constexpr int WAVES = THREADS / 64;
 constexpr float LOG2E = 1.4426950408889634f;
 constexpr float LN2 = 0.6931471805599453f;
-constexpr float LOWEST = -3.402823466e38f;
 constexpr int LIST = 1024;                 // candidates held in LDS
 constexpr int BLOCK_VECS = 8;              // vectors per entry of the block maxima: the eight lanes three DPP steps join
 constexpr int PART_VECS_MAX = 32768;       // 16 KB of block maxima
@@ -39,22 +39,39 @@ typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 
 __device__ __forceinline__ float ex2(float x) { return __builtin_amdgcn_exp2f(x); }     // arguments <= 0: what flushes to 0 is 0 in a sum
 
-// The maximum starts at the lowest finite number (entries at -inf then give differences that are numbers or -inf).  A term far
-// below the maximum is 0 in s and, its difference cut at -200, a zero in u as well.  NaN passes the maxima and stays in s.
-struct Stat { float m, s, u; };
-constexpr float FAR = -200.f;
+// r starts below every row that this form is for: a row whose r ends up past +-EXTREME (logits of the type's lowest value
+// throughout, or near its largest, where x itself overflows) is done again by far_row.  A term far below r is 0 in s and, its exponent
+// cut at FAR, a zero in u as well.  NaN passes the maxima and stays in s.
+struct Stat { float r, s, u; };
+constexpr float START = -1e30f, EXTREME = 1e29f, FAR = -300.f;
 
-__device__ __forceinline__ void raise(Stat& st, float m) {
-  const float d = st.m - m, f = ex2(d * LOG2E);
+__device__ __forceinline__ void raise(Stat& st, float r) {
+  const float d = st.r - r, f = ex2(d);
   st.u = f * (st.u + st.s * fmaxf(d, FAR));
   st.s *= f;
-  st.m = m;
+  st.r = r;
 }
-__device__ __forceinline__ void add(Stat& st, float z) {
-  const float d = z - st.m, e = ex2(d * LOG2E);
-  st.s += e;
-  st.u = fmaf(e, fmaxf(d, FAR), st.u);
+// N logits whose largest is `most`
+template <int N>
+__device__ __forceinline__ void add(Stat& st, const float (&z)[N], float most) {
+  const float top = most * LOG2E;
+  if (top > st.r) raise(st, ceilf(top));
+  float x[N], e[N], u = 0.f;
+#pragma unroll
+  for (int i = 0; i < N; i++) {
+    x[i] = fmaf(z[i], LOG2E, -st.r);
+    e[i] = ex2(x[i]);
+    st.s += e[i];
+    u = fmaf(e[i], x[i], u);
+  }
+  if (u != u) {                              // 0 times -inf (or NaN, which stays): few vectors of few rows
+    u = 0.f;
+#pragma unroll
+    for (int i = 0; i < N; i++) u = fmaf(e[i], fmaxf(x[i], FAR), u);
+  }
+  st.u += u;
 }
+
 template <typename T> struct Row;
 template <> struct Row<__hip_bfloat16> {
   static constexpr int EPV = 8;
@@ -129,20 +146,62 @@ struct Shared {
 
 // The workgroup's sums from the threads': raised to the wave's maximum and added, then the same for the waves.
 __device__ Stat join(Shared& sh, Stat st) {
-  raise(st, wave_all(st.m, [](float a, float b) { return fmaxf(a, b); }));
+  raise(st, wave_all(st.r, [](float a, float b) { return fmaxf(a, b); }));
   st.s = wave_all(st.s, [](float a, float b) { return a + b; });
   st.u = wave_all(st.u, [](float a, float b) { return a + b; });
   if ((threadIdx.x & 63) == 0) sh.part[threadIdx.x >> 6] = st;
   __syncthreads();
-  Stat all = {sh.part[0].m, 0.f, 0.f};
-  for (int w = 1; w < WAVES; w++) all.m = fmaxf(all.m, sh.part[w].m);
+  Stat all = {sh.part[0].r, 0.f, 0.f};
+  for (int w = 1; w < WAVES; w++) all.r = fmaxf(all.r, sh.part[w].r);
   for (int w = 0; w < WAVES; w++) {
     Stat p = sh.part[w];
-    raise(p, all.m);
+    raise(p, all.r);
     all.s += p.s;
     all.u += p.u;
   }
   return all;
+}
+
+// What a row's outputs are made of: ln p of a logit is ln 2 ((x - r) - log2 s), or, for a row of extreme logits, (z - m) - ln s.
+struct Result {
+  bool far;
+  float ref, log_s, entropy;                 // r or m; log2 s or ln s
+  __device__ __forceinline__ float lse() const { return far ? ref + log_s : LN2 * (ref + log_s); }
+  __device__ __forceinline__ float logp(float z) const {
+    if (far) return (z - ref) - log_s;
+    if (!(fabsf(z) < EXTREME)) return z - lse();          // a masked logit, whose x overflows
+    return LN2 * (fmaf(z, LOG2E, -ref) - log_s);
+  }
+};
+
+// The sums of a row of extreme logits against its maximum, differences taken before they are scaled: two more passes.
+template <typename T>
+__device__ Result far_row(Shared& sh, const T* row, int vocab) {
+  const int t = threadIdx.x;
+  float m = -INFINITY;
+  for (int e = t; e < vocab; e += THREADS) m = fmaxf(m, Row<T>::at(row, e));
+  m = wave_all(m, [](float a, float b) { return fmaxf(a, b); });
+  __syncthreads();                           // (the sums in sh.part have been read)
+  if ((t & 63) == 0) sh.part[t >> 6].r = m;
+  __syncthreads();
+  for (int w = 0; w < WAVES; w++) m = fmaxf(m, sh.part[w].r);
+  Stat st = {0.f, 0.f, 0.f};
+  for (int e = t; e < vocab; e += THREADS) {
+    const float d = Row<T>::at(row, e) - m, p = ex2(d * LOG2E);
+    st.s += p;
+    st.u = fmaf(p, fmaxf(d, FAR), st.u);
+  }
+  __syncthreads();
+  st = join(sh, st);
+  const float ln_s = LN2 * log2f(st.s);
+  return {true, m, ln_s, ln_s - st.u / st.s};
+}
+
+template <typename T>
+__device__ __forceinline__ Result result_of(Shared& sh, const Stat& all, const T* row, int vocab) {
+  if (!(fabsf(all.r) < EXTREME)) return far_row(sh, row, vocab);          // (all threads hold the same r)
+  const float log_s = log2f(all.s);
+  return {false, all.r, log_s, LN2 * (log_s - all.u / all.s)};
 }
 
 // Bound from the threads' largest entries (order_of; 0 = none): the largest multiple T of 2^16 that at least k of them reach.
@@ -239,13 +298,12 @@ entropy_rows_kernel(int64_t row0, int vocab, const T* __restrict__ logits, int64
   const bool first = part == 0, last = part == parts - 1;
   const u32x4* vp = reinterpret_cast<const u32x4*>(row + head);
 
-  Stat st = {LOWEST, 0.f, 0.f};
+  Stat st = {START, 0.f, 0.f};
   [[maybe_unused]] float top = -INFINITY;                  // largest of the thread's entries
   auto single = [&](int e) {
-    const float z = Row<T>::at(row, e);
-    if (TOP) top = fmaxf(top, z);
-    if (z > st.m) raise(st, z);
-    add(st, z);
+    const float z[1] = {Row<T>::at(row, e)};
+    if (TOP) top = fmaxf(top, z[0]);
+    add<1>(st, z, z[0]);
   };
   auto vec = [&](const u32x4& v, int i) {
     float z[EPV];
@@ -258,9 +316,7 @@ entropy_rows_kernel(int64_t row0, int vocab, const T* __restrict__ logits, int64
       const float bm = max8(vm);
       if ((t & 7) == 0) block_max[(i - v0) / BLOCK_VECS] = bm;
     }
-    if (vm > st.m) raise(st, vm);
-#pragma unroll
-    for (int e = 0; e < EPV; e++) add(st, z[e]);
+    add<EPV>(st, z, vm);
   };
   if (first) for (int e = t; e < head; e += THREADS) single(e);
   // Rounds of 256 vectors, four in flight.  Of the last four, those past the end are left out, and in the ragged one all lanes take
@@ -291,17 +347,18 @@ entropy_rows_kernel(int64_t row0, int vocab, const T* __restrict__ logits, int64
   if (last) for (int e = tail0 + t; e < vocab; e += THREADS) single(e);
 
   const Stat all = join(sh, st);
-  const float ln_s = LN2 * log2f(all.s);
-  if (t == 0) {
-    if (parts == 1) {
+  Result res{};
+  if (parts == 1) {
+    res = result_of(sh, all, row, vocab);
+    if (t == 0) {
       const int y = target[r];
       const bool used = y >= 0 && y < vocab;
-      out.logp[r] = used ? (Row<T>::at(row, y) - all.m) - ln_s : 0.f;
-      out.entropy[r] = used ? ln_s - all.u / all.s : 0.f;
-      if (out.lse) out.lse[r] = all.m + ln_s;
-    } else {
-      partial[r * parts + part].st = all;
+      out.logp[r] = used ? res.logp(Row<T>::at(row, y)) : 0.f;
+      out.entropy[r] = used ? res.entropy : 0.f;
+      if (out.lse) out.lse[r] = res.lse();
     }
+  } else if (t == 0) {
+    partial[r * parts + part].st = all;
   }
   if constexpr (TOP) {
     const bool any = (v0 + t < v1) || (first && t < head) || (last && tail0 + t < vocab);
@@ -345,7 +402,7 @@ entropy_rows_kernel(int64_t row0, int vocab, const T* __restrict__ logits, int64
     auto emit = [&](int rank, Key key) {
       if (parts == 1) {
         out.top_index[r * k + rank] = (int32_t)~(uint32_t)key;
-        out.top_logp[r * k + rank] = (value_of((uint32_t)(key >> 32)) - all.m) - ln_s;
+        out.top_logp[r * k + rank] = res.logp(value_of((uint32_t)(key >> 32)));
       } else {
         keys[(r * parts + part) * k + rank] = key;          // 0 where the part has fewer than k entries
       }
@@ -362,23 +419,24 @@ entropy_join_kernel(int64_t row0, int vocab, const T* __restrict__ logits, int64
   __shared__ Shared sh;
   const int64_t r = row0 + blockIdx.x;
   const int t = threadIdx.x;
-  Stat st = {LOWEST, 0.f, 0.f};
+  Stat st = {START, 0.f, 0.f};
   for (int p = t; p < parts; p += THREADS) {
     Stat q = partial[r * parts + p].st;
-    const float m = fmaxf(st.m, q.m);
+    const float m = fmaxf(st.r, q.r);
     raise(st, m);
     raise(q, m);
     st.s += q.s;
     st.u += q.u;
   }
   const Stat all = join(sh, st);
-  const float ln_s = LN2 * log2f(all.s);
+  const T* row = logits + r * row_stride;
+  const Result res = result_of(sh, all, row, vocab);
   if (t == 0) {
     const int y = target[r];
     const bool used = y >= 0 && y < vocab;
-    out.logp[r] = used ? (Row<T>::at(logits + r * row_stride, y) - all.m) - ln_s : 0.f;
-    out.entropy[r] = used ? ln_s - all.u / all.s : 0.f;
-    if (out.lse) out.lse[r] = all.m + ln_s;
+    out.logp[r] = used ? res.logp(Row<T>::at(row, y)) : 0.f;
+    out.entropy[r] = used ? res.entropy : 0.f;
+    if (out.lse) out.lse[r] = res.lse();
   }
   if constexpr (TOP) {
     const Key* mine = keys + r * parts * k;
@@ -396,7 +454,7 @@ entropy_join_kernel(int64_t row0, int vocab, const T* __restrict__ logits, int64
         },
         [&](int rank, Key key) {
           out.top_index[r * k + rank] = (int32_t)~(uint32_t)key;
-          out.top_logp[r * k + rank] = (value_of((uint32_t)(key >> 32)) - all.m) - ln_s;
+          out.top_logp[r * k + rank] = res.logp(value_of((uint32_t)(key >> 32)));
         });
   }
 }

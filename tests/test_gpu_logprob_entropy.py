@@ -155,6 +155,37 @@ def test_rows_without_a_distribution_and_ignored_rows(n):
     torch.cuda.synchronize()
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("n", [2, 530])
+def test_logits_near_the_ends_of_the_type(n, dtype):
+    """Rows that overflow when scaled to powers of two: equal largest logits share the probability, everything below them (a step of
+    the type is more than 10^29 there) has none."""
+    vocab = 2500
+    for top, rest in ((3.2e38, 3.0e38), (-3.0e38, -3.2e38), (2.4e38, -2.4e38), (-3.2e38, -float("inf")), (1e30, 0.0), (-1e30, -2e30)):
+        z = torch.full((n, vocab), rest).to(DT[dtype]).cuda()
+        z[:, 700:704] = top
+        y = torch.full((n,), 702, dtype=torch.int32, device="cuda")
+        y[1] = 5
+        logp, ent, lse, idx, tl = T.tree_logprob_entropy(z, y, top_k=6)
+        assert torch.allclose(logp[0], torch.tensor(-math.log(4.0)).cuda(), atol=1e-6) and torch.allclose(ent, torch.tensor(math.log(4.0)).cuda(), atol=1e-6)
+        assert (lse - z[:, 700].float()).abs().max() <= 2.0 ** -22 * abs(top)
+        assert idx[0].tolist() == [700, 701, 702, 703, 0, 1]
+        assert torch.allclose(tl[:, :4], torch.tensor(-math.log(4.0)).cuda(), atol=1e-6) and (tl[:, 4:] < -1e28).all() and logp[1] < -1e28
+        g = T.tree_logprob_entropy_bwd(z, y, lse, ent, torch.ones(n, device="cuda"))
+        assert torch.isfinite(g).all()
+    torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("shift", [-5000.0, 3000.0])
+def test_a_common_shift_changes_nothing_but_lse(shift):
+    """In fp32, logits on a grid of 2^-8 so that the shifted ones are exact."""
+    z = (torch.randn(40, 6001, generator=torch.Generator().manual_seed(4)) * 512).round().cuda() / 256
+    y = torch.arange(40, dtype=torch.int32, device="cuda")
+    a, b = T.tree_logprob_entropy(z, y, top_k=9), T.tree_logprob_entropy(z + shift, y, top_k=9)
+    check(z + shift, y, 9, b)
+    assert (a[0] - b[0]).abs().max() <= 4e-6 and (a[1] - b[1]).abs().max() <= 4e-6 and torch.equal(a[3], b[3])
+
+
 def want_grad(z, y, a, b):
     zf = z.double().cpu().numpy()
     logp, ent, lse, _, _ = want(z, y, 0)
