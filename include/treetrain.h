@@ -415,7 +415,7 @@ tt_status tt_tree_rope(int64_t n_tokens, int32_t n_heads, int32_t d, int32_t dty
  * The terms of a policy-gradient objective, per row r of the logits: lse_r = ln sum_v exp(z_rv),
  * logp_r = z_r[target_r] - lse_r, entropy_r = -sum_v p_rv ln p_rv with p = softmax(z_r), and the top_k
  * most probable entries.  The logits are read once.
- *   logits, target as for tt_tree_weighted_logprob.  A row whose target is negative or >= vocab is
+ *   logits, target as for tt_tree_weighted_logprob; vocab at most 2^30.  A row whose target is negative or >= vocab is
  *     ignored: logp = 0 and entropy = 0, and its gradient is zero (lse and the alternatives are still
  *     written).
  *   top_k in [0, min(64, vocab)].  top_index, top_logp [n_rows][top_k]: indices in order of falling

@@ -634,6 +634,14 @@ def _enter_device(*tensors):
     return before
 
 
+def _new(shape, dtype, device, stream):
+    """An empty tensor for a call on `stream` (None: the current one): not reused, once dropped, before that stream is through."""
+    t = _TORCH.empty(shape, dtype=dtype, device=device)
+    if stream is not None:
+        t.record_stream(stream)
+    return t
+
+
 def _leave_device(before):
     if before is not None:
         _torch().cuda.set_device(before)
@@ -760,7 +768,7 @@ def tree_rope_axes(x, axis_pos, sections, *, interleaved: bool = False, theta_ba
     before = _enter_device(x, axis_pos, out)
     try:
         if out is None:
-            out = torch.empty((n, h, d), dtype=x.dtype, device=x.device)
+            out = _new((n, h, d), x.dtype, x.device, stream)
         _check(_lib().tt_tree_rope_axes(n, h, d, DTYPE_BF16 if x.dtype == torch.bfloat16 else DTYPE_FP32, _dp(x), stride, n_axes,
                                         _dp(axis_pos), pair_axis, float(theta_base), 1 if inverse else 0, _dp(out), out_stride,
                                         _stream_ptr(stream)))
@@ -830,7 +838,7 @@ def tree_logprob_entropy(logits, target, *, top_k: int = 0, logp=None, entropy=N
     before = _enter_device(logits, target, logp, entropy, lse, top_index, top_logp, workspace)
     try:
         dev = logits.device
-        new = lambda *shape, dtype=torch.float32: torch.empty(shape, dtype=dtype, device=dev)      # noqa: E731
+        new = lambda *shape, dtype=torch.float32: _new(shape, dtype, dev, stream)      # noqa: E731
         logp, entropy, lse = (new(n) if t is None else t for t in (logp, entropy, lse))
         if top_k:
             top_index = new(n, top_k, dtype=torch.int32) if top_index is None else top_index
@@ -864,7 +872,7 @@ def tree_logprob_entropy_bwd(logits, target, lse, entropy, d_logp=None, d_entrop
     before = _enter_device(logits, target, lse, entropy, d_logp, d_entropy, out)
     try:
         if out is None:
-            out = torch.empty((n, vocab), dtype=logits.dtype, device=logits.device)
+            out = _new((n, vocab), logits.dtype, logits.device, stream)
         _check(_lib().tt_tree_logprob_entropy_bwd(n, vocab, code, _dp(logits), stride, _dp(target), _dp(lse), _dp(entropy),
                                                   _dp(d_logp), _dp(d_entropy), _dp(out), out_stride, _stream_ptr(stream)))
     finally:
@@ -1196,11 +1204,11 @@ def tree_scan_fwd(x, dt, A, B, C, plan: GdnPlan, *, D=None, z=None, dt_bias=None
         captured = return_states and plan.n_capture > 0
         chunks = plan._scan_chunks(ch, False, dev, captured)
         if out is None:
-            out = torch.empty((n, ch), dtype=x.dtype, device=dev)
-        states = torch.empty((plan.n_capture, ch, m), dtype=torch.float32, device=dev) if return_states else None
+            out = _new((n, ch), x.dtype, dev, stream)
+        states = _new((plan.n_capture, ch, m), torch.float32, dev, stream) if return_states else None
         need = int(_lib().tt_tree_scan_fwd_workspace(ctypes.byref(desc), chunks.n_chunks, chunks.n_slots))
         if workspace is None:
-            workspace = torch.empty(max(need, 256), dtype=torch.uint8, device=dev)
+            workspace = _new(max(need, 256), torch.uint8, dev, stream)
         _check(_lib().tt_tree_scan_fwd(ctypes.byref(desc), ctypes.byref(chunks), _dp(x), _dp(dt), _dp(A), _dp(B), _dp(C), _dp(D), _dp(z),
                                        _dp(dt_bias), _dp(initial_state), _dp(states) if captured else None, _dp(out), _dp(workspace),
                                        workspace.numel() * workspace.element_size(), _stream_ptr(stream)))
@@ -1236,11 +1244,11 @@ def tree_scan_bwd(x, dt, A, B, C, d_y, plan: GdnPlan, *, D=None, z=None, dt_bias
         dev = x.device
         captured = d_state_out is not None and plan.n_capture > 0
         chunks = plan._scan_chunks(ch, True, dev, captured)
-        like = lambda t: None if t is None else torch.empty(t.shape, dtype=t.dtype, device=dev)      # noqa: E731
+        like = lambda t: None if t is None else _new(t.shape, t.dtype, dev, stream)      # noqa: E731
         grads = ScanGrads(like(x), like(x), like(A), like(B), like(C), like(D), like(z), like(dt_bias), like(A) if want_d_initial_state else None)
         need = int(_lib().tt_tree_scan_bwd_workspace(ctypes.byref(desc), chunks.n_chunks, chunks.n_slots))
         if workspace is None:
-            workspace = torch.empty(max(need, 256), dtype=torch.uint8, device=dev)
+            workspace = _new(max(need, 256), torch.uint8, dev, stream)
         _check(_lib().tt_tree_scan_bwd(ctypes.byref(desc), ctypes.byref(chunks), _dp(x), _dp(dt), _dp(A), _dp(B), _dp(C), _dp(D), _dp(z),
                                        _dp(dt_bias), _dp(initial_state), _dp(d_y), _dp(d_state_out) if captured else None,
                                        *(_dp(g) for g in grads), _dp(workspace), workspace.numel() * workspace.element_size(),
@@ -1269,9 +1277,9 @@ def tree_scan_step(x, dt, A, B, C, state, *, index=None, D=None, z=None, dt_bias
     before = _enter_device(x, dt, A, B, C, D, z, dt_bias, state, index, state_out, out)
     try:
         if out is None:
-            out = torch.empty((n, ch), dtype=x.dtype, device=x.device)
+            out = _new((n, ch), x.dtype, x.device, stream)
         if state_out is None:
-            state_out = torch.empty((n, ch, m), dtype=torch.float32, device=x.device)
+            state_out = _new((n, ch, m), torch.float32, x.device, stream)
         _check(_lib().tt_tree_scan_step(ctypes.byref(desc), _dp(x), _dp(dt), _dp(A), _dp(B), _dp(C), _dp(D), _dp(z), _dp(dt_bias), slots,
                                         _dp(state), _dp(index), _dp(state_out), _dp(out), _stream_ptr(stream)))
     finally:
@@ -1302,9 +1310,9 @@ def tree_conv_step(x, state, weight, bias=None, *, index=None, silu: bool = True
     before = _enter_device(x, state, weight, bias, index, state_out, out)
     try:
         if out is None:
-            out = torch.empty((n, c), dtype=x.dtype, device=x.device)
+            out = _new((n, c), x.dtype, x.device, stream)
         if state_out is None:
-            state_out = torch.empty((n, k - 1, c), dtype=x.dtype, device=x.device)
+            state_out = _new((n, k - 1, c), x.dtype, x.device, stream)
         _check(_lib().tt_tree_conv_step(n, c, k, DTYPE_BF16 if x.dtype == torch.bfloat16 else DTYPE_FP32, 1 if silu else 0, _dp(x), xs,
                                         _dp(weight), _dp(bias), slots, _dp(state), _dp(index), _dp(state_out), _dp(out), ys,
                                         _stream_ptr(stream)))

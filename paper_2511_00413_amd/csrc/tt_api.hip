@@ -1,7 +1,6 @@
 // C ABI entry points of the device calls: argument validation on the host, then dispatch to the
 // kernels.  Nothing is launched unless every check passes.
 #include <hip/hip_runtime.h>
-#include <algorithm>
 #include <climits>
 #include <cmath>
 #include <mutex>
@@ -255,24 +254,24 @@ extern "C" tt_status tt_tree_rope(int64_t n_tokens, int32_t n_heads, int32_t d, 
 }
 
 namespace {
-// Whether two arrays of `rows` rows of `len` bytes share memory.  Rows that interleave (slices of one buffer) do not; with unequal
-// steps the whole extents decide.
-bool shares_memory(const void* a, int64_t step_a, const void* b, int64_t step_b, int64_t len, int64_t rows) {
+// Whether two arrays of `rows` rows (of len_a and len_b bytes) share memory.  Rows that interleave (slices of one buffer) do not; with
+// unequal steps the whole extents decide.
+bool shares_memory(const void* a, int64_t step_a, int64_t len_a, const void* b, int64_t step_b, int64_t len_b, int64_t rows) {
   if (rows <= 0) return false;
   const uintptr_t a0 = reinterpret_cast<uintptr_t>(a), b0 = reinterpret_cast<uintptr_t>(b);
   if (step_a == step_b) {
     const int64_t off = (int64_t)(b0 - a0), part = ((off % step_a) + step_a) % step_a, q = (off - part) / step_a;
-    // row i of b starts `part` bytes into row i + q of a
-    return (part < len && q > -rows && q < rows) || (step_a - part < len && q + 1 > -rows && q + 1 < rows);
+    // row i of b starts `part` bytes into row i + q of a, and step - part bytes in front of row i + q + 1
+    return (part < len_a && q > -rows && q < rows) || (step_a - part < len_b && q + 1 > -rows && q + 1 < rows);
   }
-  const uintptr_t a1 = a0 + (uintptr_t)((rows - 1) * step_a + len), b1 = b0 + (uintptr_t)((rows - 1) * step_b + len);
+  const uintptr_t a1 = a0 + (uintptr_t)((rows - 1) * step_a + len_a), b1 = b0 + (uintptr_t)((rows - 1) * step_b + len_b);
   return a0 < b1 && b0 < a1;
 }
 
 tt_status check_entropy(int64_t n_rows, int32_t vocab, int32_t dtype) {
   if (dtype != TT_DTYPE_BF16 && dtype != TT_DTYPE_FP32) return fail(TT_ERR_DTYPE, "unknown dtype %d", dtype);
   if (n_rows < 0 || n_rows > 0x7fffffffLL) return fail(TT_ERR_SHAPE, "n_rows=%lld out of range", (long long)n_rows);
-  if (vocab <= 0) return fail(TT_ERR_SHAPE, "vocab=%d must be positive", vocab);
+  if (vocab <= 0 || vocab > 1 << 30) return fail(TT_ERR_SHAPE, "vocab=%d must lie in [1, 2^30]", vocab);
   return TT_OK;
 }
 tt_status check_top_k(int32_t vocab, int32_t top_k) {
@@ -326,7 +325,7 @@ extern "C" tt_status tt_tree_logprob_entropy_bwd(int64_t n_rows, int32_t vocab, 
   if (reinterpret_cast<uintptr_t>(logits) % es || reinterpret_cast<uintptr_t>(dlogits) % es)
     return fail(TT_ERR_ALIGN, "logits / dlogits is not aligned to its element size");
   if (!(dlogits == logits && dlogits_row_stride == row_stride) &&
-      shares_memory(logits, row_stride * es, dlogits, dlogits_row_stride * es, vocab * es, n_rows))
+      shares_memory(logits, row_stride * es, vocab * es, dlogits, dlogits_row_stride * es, vocab * es, n_rows))
     return fail(TT_ERR_SHAPE, "dlogits may share memory with logits only as a whole, with equal row strides");
   return hip_result(tt::logprob_entropy_bwd(n_rows, vocab, dtype == TT_DTYPE_BF16, logits, row_stride, target, lse, entropy, d_logp,
                                             d_entropy, dlogits, dlogits_row_stride, (hipStream_t)stream),
@@ -356,7 +355,7 @@ extern "C" tt_status tt_tree_rope_axes(int64_t n_tokens, int32_t n_heads, int32_
   if (n_tokens > 0 && (!x || !y || !axis_pos)) return fail(TT_ERR_NULL, "x / y / axis_pos is NULL");
   if (!tt::aligned16(x) || !tt::aligned16(y)) return fail(TT_ERR_ALIGN, "x / y is not 16-byte aligned");
   const int64_t es = dtype == TT_DTYPE_BF16 ? 2 : 4, len = (int64_t)n_heads * d * es;
-  if (!(x == y && x_stride_tok == y_stride_tok) && shares_memory(x, x_stride_tok * es, y, y_stride_tok * es, len, n_tokens))
+  if (!(x == y && x_stride_tok == y_stride_tok) && shares_memory(x, x_stride_tok * es, len, y, y_stride_tok * es, len, n_tokens))
     return fail(TT_ERR_SHAPE, "y may share memory with x only as a whole, with equal token strides");
   return hip_result(tt::rope_axes(n_tokens, n_heads, d, dtype == TT_DTYPE_BF16, x, x_stride_tok, axis_pos, pair_axis, theta_base,
                                   inverse != 0, y, y_stride_tok, (hipStream_t)stream),
@@ -641,8 +640,8 @@ struct Rows {
 // Whether an output lies on an input: exact for rows of equal step (slices of one buffer), by their extents otherwise.
 bool meets(const Rows& a, const Rows& b) {
   if (!a.p || !b.p || a.n <= 0 || b.n <= 0) return false;
-  if (a.step == b.step && a.n == b.n) return shares_memory(a.p, a.step * a.es, b.p, b.step * b.es, std::max(a.len, b.len) * a.es, a.n);
-  return meets(a.span(), b.span());
+  if (a.n != b.n) return meets(a.span(), b.span());
+  return shares_memory(a.p, a.step * a.es, a.len * a.es, b.p, b.step * b.es, b.len * b.es, a.n);
 }
 
 bool aligned_to(const void* p, size_t n) { return reinterpret_cast<uintptr_t>(p) % n == 0; }

@@ -158,6 +158,11 @@ struct Program {
   }
   static __device__ __forceinline__ int at(int v, int u) { return __builtin_amdgcn_readlane(v, u & 63); }
 };
+// Whether a wave of a walk has no entry at all.  In one that has some, the lanes past the last entry stand in for it, in step with the
+// lane that is on it: they write what it writes.  A whole wave of such lanes would not be in step and add to the saved gradients again.
+__device__ __forceinline__ bool walk_is_empty(int64_t width) {
+  return (int64_t)blockIdx.x * WALK_THREADS + (int64_t)(threadIdx.x & ~63u) >= width;
+}
 template <bool LDS>
 struct Slots {
   float* p;
@@ -193,7 +198,6 @@ struct WalkRows {
 };
 
 // Down the tree: replaces add[chunk] by the state entering the chunk.  leave(cap, state) sees the captured states.
-// (Lanes past the last entry stand in for it: they write what it writes.)
 template <bool LDS, typename Leave>
 __device__ __forceinline__ void walk_down(const ScanArgs& a, float* local, const float* __restrict__ steps, int64_t width, int64_t at, int c,
                                           float a2, float first, const Slots<LDS>& slots, bool with_cap, Leave leave) {

@@ -67,6 +67,7 @@ __global__ void __launch_bounds__(WALK_THREADS)
 scan_states_kernel(ScanArgs a, float* local, const float* __restrict__ steps, float* saved) {
   extern __shared__ float lds[];
   const int64_t width = (int64_t)a.n_state * a.channels;
+  if (walk_is_empty(width)) return;
   const int64_t at = min((int64_t)blockIdx.x * WALK_THREADS + threadIdx.x, width - 1);
   const int n = (int)(at / a.channels), c = (int)(at - (int64_t)n * a.channels);
   const int64_t state_at = (int64_t)c * a.n_state + n;

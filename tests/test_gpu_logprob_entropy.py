@@ -271,3 +271,17 @@ def test_interleaved_slices_of_one_buffer():
     assert torch.equal(T.tree_logprob_entropy_bwd(z, y, lse, ent, one, one, out=out), want_g)
     with pytest.raises(T.TreeTrainError):
         T.tree_logprob_entropy_bwd(z, y, lse, ent, one, one, out=buf[:, 256:768])
+
+
+def test_given_outputs_and_workspace():
+    z, y = make(3, 70001, "bf16", 8)
+    need = T.tree_logprob_entropy_workspace(z, 11)
+    ws = torch.full((need + 1024,), 77, dtype=torch.uint8, device="cuda")
+    out = [torch.full((3,), 5.0, device="cuda") for _ in range(3)]
+    idx, top = torch.zeros(3, 11, dtype=torch.int32, device="cuda"), torch.zeros(3, 11, device="cuda")
+    got = T.tree_logprob_entropy(z, y, top_k=11, logp=out[0], entropy=out[1], lse=out[2], top_index=idx, top_logp=top, workspace=ws)
+    torch.cuda.synchronize()
+    assert got[0] is out[0] and got[3] is idx and (ws[need:] == 77).all()
+    check(z, y, 11, got)
+    with pytest.raises(T.TreeTrainError):
+        T.tree_logprob_entropy(z, y, top_k=11, workspace=ws[:need - 1])

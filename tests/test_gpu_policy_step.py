@@ -224,3 +224,19 @@ def test_tensors_off_the_gpu_are_refused():
         T.tree_scan_fwd(x, x, A, Bc, Bc, plan)
     with pytest.raises(ValueError):
         T.tree_logprob_entropy(x, torch.zeros(6, dtype=torch.int32))
+
+
+def test_a_given_stream_while_another_is_current():
+    """Temporaries of a call on a given stream are not handed out again while that stream still works on them."""
+    _, step = all_calls(torch.float32)
+    want = [t.clone() for t in step()]
+    torch.cuda.synchronize()
+    other = torch.cuda.Stream()
+    for _ in range(3):
+        other.wait_stream(torch.cuda.current_stream())                # (the memory may have been the current stream's until now)
+        got = step(stream=other)
+        for size in (1 << 20, 1 << 22, 1 << 24):                      # the current stream takes and fills memory of all sizes
+            torch.full((size,), float("nan"), device="cuda")
+    torch.cuda.synchronize()
+    for i, (a, b) in enumerate(zip(got, want)):
+        assert torch.equal(a, b), i

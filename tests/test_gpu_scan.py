@@ -242,3 +242,33 @@ def test_extreme_steps():
     R.assert_close(y, yy, size["y"], n, m, 2.0 ** -24, "y")
     for name, adds in (("dx", m), ("ddt", m), ("dA", n), ("dB", ch), ("dC", ch), ("dD", n)):
         R.assert_close(getattr(g, name), ins[name[1:]].grad, size[name], 2 * n, adds, 2.0 ** -24, name)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("ch", [6, 70])
+def test_more_branch_points_than_fit_on_chip(ch, dtype):
+    """A binary tree of 511 nodes has 255 branch points, whose states are kept in the workspace; 6 x 16 and 70 x 16 states leave lanes
+    and whole waves of a workgroup without an entry."""
+    parent = [-1] + [(i - 1) // 2 for i in range(1, 511)]
+    TREES["binary"] = (parent, [1 + i % 2 for i in range(511)])
+    run_case("binary", ch, 16, 1, dtype, gateway=True)
+    assert T.tree_gdn_plan(*TREES["binary"]).n_slots == 255
+
+
+def test_given_workspaces_are_not_overrun():
+    parent, seg = TREES["worked"]
+    n, ch = sum(seg), 200
+    d = cuda(make(n, ch, 8, 1, torch.bfloat16, 6))
+    args, layer = [d[i] for i in ("x", "dt", "A", "B", "C")], {i: d[i] for i in ("D", "z", "dt_bias")}
+    plan = T.tree_gdn_plan(parent, seg)
+    for back in (False, True):
+        need = T.tree_scan_workspace(d["x"], d["A"], d["B"], plan, backward=back)
+        ws = torch.full((need + 4096,), 77, dtype=torch.uint8, device="cuda")
+        call = (lambda w: T.tree_scan_bwd(*args, d["x"], plan, workspace=w, **layer)) if back else (lambda w: T.tree_scan_fwd(*args, plan, workspace=w, **layer))
+        a, b = call(ws), call(None)
+        for p, q in zip(a, b) if back else [(a, b)]:
+            assert p is q or torch.equal(p, q)
+        assert (ws[need:] == 77).all()
+        with pytest.raises(T.TreeTrainError):
+            call(ws[:need - 1])
+    torch.cuda.synchronize()
