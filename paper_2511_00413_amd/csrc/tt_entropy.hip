@@ -7,12 +7,11 @@
 // is one fused multiply-add with a single rounding, and the differences lose nothing.  Gradient of d_logp logp + d_entropy entropy:
 //   dz_v = d_logp ([v = y] - p_v) - d_entropy p_v (ln p_v + entropy).
 //
-// Top alternatives without a second pass: in the same pass the maximum of every block of eight 16-byte vectors goes to LDS.
-// The k-th largest of the threads' own maxima is a lower bound of the k-th largest entry (k threads hold an entry that large),
-// so only the blocks that reach it are read again: a little more than k blocks of 128 bytes.  Keys are 64 bits -- the value in an
-// order of whole numbers above the complement of the index -- so no two are equal, ties go to the lowest index, and the order in
-// which candidates are collected does not matter.  Where more candidates tie at the bound than the list holds, the row is read
-// again once per alternative.
+// Top alternatives without a second pass: in the same pass every thread leaves the maximum of each four of its vectors in LDS.  The
+// k-th largest of the threads' own maxima is a lower bound of the k-th largest entry (k threads hold an entry that large), so only the
+// vectors that reach it are read again: a little more than k times four.  Keys are 64 bits -- the value in an order of whole numbers
+// above the complement of the index -- so no two are equal, ties go to the lowest index, and the order in which candidates are
+// collected does not matter.  Where more candidates tie at the bound than the list holds, the row is read again once per alternative.
 //
 // Bound by HBM: every logit is read once.  Few rows are cut into parts for one workgroup each, joined by a second launch.
 #include <hip/hip_runtime.h>
@@ -29,8 +28,8 @@ constexpr int WAVES = THREADS / 64;
 constexpr float LOG2E = 1.4426950408889634f;
 constexpr float LN2 = 0.6931471805599453f;
 constexpr int LIST = 1024;                 // candidates held in LDS
-constexpr int BLOCK_VECS = 8;              // vectors per entry of the block maxima: the eight lanes three DPP steps join
-constexpr int PART_VECS_MAX = 32768;       // 16 KB of block maxima
+constexpr int ROUNDS = 4;                  // a thread's vectors per entry of the maxima kept in LDS: 4 bytes per 64 of the row
+constexpr int PART_VECS_MAX = 32768;       // 32 KB of them
 constexpr int64_t LAUNCH_GROUPS = 1 << 22; // workgroups per launch: a dimension holds less than 2^32 work-items
 
 typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
@@ -117,11 +116,6 @@ __device__ __forceinline__ Key key_of(float z, int index) { return (Key)order_of
 template <int CTRL>
 __device__ __forceinline__ float dpp(float v) { return __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(v), CTRL, 0xf, 0xf, true)); }
 constexpr int XOR1 = 0xb1, XOR2 = 0x4e, HALF_MIRROR = 0x141, ROR8 = 0x128;
-__device__ __forceinline__ float max8(float v) {                 // over the lane's group of eight
-  v = fmaxf(v, dpp<XOR1>(v));
-  v = fmaxf(v, dpp<XOR2>(v));
-  return fmaxf(v, dpp<HALF_MIRROR>(v));
-}
 template <typename Op>
 __device__ __forceinline__ float wave_all(float v, Op op) {       // over the wave
   v = op(v, dpp<XOR1>(v));
@@ -286,7 +280,7 @@ entropy_rows_kernel(int64_t row0, int vocab, const T* __restrict__ logits, int64
                     int k, int parts, int part_vecs, Outs out, Partial* __restrict__ partial, Key* __restrict__ keys) {
   constexpr int EPV = Row<T>::EPV;
   __shared__ Shared sh;
-  extern __shared__ float block_max[];
+  extern __shared__ float four_max[];
   const int64_t r = row0 + (parts == 1 ? (int64_t)blockIdx.x : (int64_t)(blockIdx.x / (unsigned)parts));
   const int part = parts == 1 ? 0 : (int)(blockIdx.x % (unsigned)parts);
   const T* row = logits + r * row_stride;
@@ -305,22 +299,21 @@ entropy_rows_kernel(int64_t row0, int vocab, const T* __restrict__ logits, int64
     if (TOP) top = fmaxf(top, z[0]);
     add<1>(st, z, z[0]);
   };
-  auto vec = [&](const u32x4& v, int i) {
+  auto vec = [&](const u32x4& v) {
     float z[EPV];
     Row<T>::unpack(v, z);
     float vm = z[0];
 #pragma unroll
     for (int e = 1; e < EPV; e++) vm = fmaxf(vm, z[e]);
-    if constexpr (TOP) {
-      top = fmaxf(top, vm);
-      const float bm = max8(vm);
-      if ((t & 7) == 0) block_max[(i - v0) / BLOCK_VECS] = bm;
-    }
     add<EPV>(st, z, vm);
+    return vm;
+  };
+  [[maybe_unused]] auto keep = [&](int r4, float m) {
+    top = fmaxf(top, m);
+    four_max[r4 / ROUNDS * THREADS + t] = m;
   };
   if (first) for (int e = t; e < head; e += THREADS) single(e);
-  // Rounds of 256 vectors, four in flight.  Of the last four, those past the end are left out, and in the ragged one all lanes take
-  // part (those past the end stand in with -inf), so that the joins of eight lanes always have eight.
+  // Rounds of 256 vectors, four in flight; of the last four, what lies past the end stands in as -inf.
   const int rounds = (v1 - v0 + THREADS - 1) / THREADS;
   int r4 = 0;
   for (; r4 + 4 < rounds; r4 += 4) {
@@ -329,7 +322,8 @@ entropy_rows_kernel(int64_t row0, int vocab, const T* __restrict__ logits, int64
     const u32x4 b = __builtin_nontemporal_load(vp + i + THREADS);
     const u32x4 c = __builtin_nontemporal_load(vp + i + 2 * THREADS);
     const u32x4 d = __builtin_nontemporal_load(vp + i + 3 * THREADS);
-    vec(a, i); vec(b, i + THREADS); vec(c, i + 2 * THREADS); vec(d, i + 3 * THREADS);
+    const float m0 = vec(a), m1 = vec(b), m2 = vec(c), m3 = vec(d);
+    if constexpr (TOP) keep(r4, fmaxf(fmaxf(m0, m1), fmaxf(m2, m3)));
   }
   if (r4 < rounds) {
     const uint32_t none = sizeof(T) == 2 ? 0xff80ff80u : 0xff800000u;      // -inf
@@ -340,9 +334,11 @@ entropy_rows_kernel(int64_t row0, int vocab, const T* __restrict__ logits, int64
       const int i = v0 + (r4 + j) * THREADS + t;
       if (i < v1) v[j] = __builtin_nontemporal_load(vp + i);
     }
+    float m = -INFINITY;
 #pragma unroll
     for (int j = 0; j < 4; j++)
-      if (r4 + j < rounds) vec(v[j], v0 + (r4 + j) * THREADS + t);
+      if (r4 + j < rounds) m = fmaxf(m, vec(v[j]));
+    if constexpr (TOP) keep(r4, m);
   }
   if (last) for (int e = tail0 + t; e < vocab; e += THREADS) single(e);
 
@@ -371,16 +367,30 @@ entropy_rows_kernel(int64_t row0, int vocab, const T* __restrict__ logits, int64
       };
       if (first) for (int e = t; e < head; e += THREADS) try_one(e);
       if (last) for (int e = tail0 + t; e < vocab; e += THREADS) try_one(e);
-      const float floor_value = value_of(bound);              // (bounds below -inf's give NaN, which passes every block)
-      for (int b = t >> 3; b * BLOCK_VECS < v1 - v0; b += THREADS / 8) {      // eight threads per block, one vector each
-        if (block_max[b] < floor_value) continue;
-        const int j = v0 + b * BLOCK_VECS + (t & 7);
-        if (j >= v1) continue;
-        float z[EPV];
-        Row<T>::unpack(vp[j], z);
+      const float floor_value = value_of(bound);              // (bounds below -inf's give NaN, which passes everything)
+      for (int r4 = 0; r4 < rounds; r4 += ROUNDS) {
+        if (four_max[r4 / ROUNDS * THREADS + t] < floor_value) continue;
+        const int j0 = v0 + r4 * THREADS + t;
+        const uint32_t none = sizeof(T) == 2 ? 0xff80ff80u : 0xff800000u;
+        u32x4 v[ROUNDS];
 #pragma unroll
-        for (int e = 0; e < EPV; e++)
-          if (order_of(z[e]) >= bound) offer(sh, key_of(z[e], head + j * EPV + e));
+        for (int q = 0; q < ROUNDS; q++) {
+          v[q] = u32x4{none, none, none, none};
+          if (j0 + q * THREADS < v1) v[q] = vp[j0 + q * THREADS];
+        }
+#pragma unroll 1
+        for (int q = 0; q < ROUNDS; q++) {
+          const int j = j0 + q * THREADS;
+          float z[EPV];
+          Row<T>::unpack(q == 0 ? v[0] : q == 1 ? v[1] : q == 2 ? v[2] : v[3], z);
+          float m = z[0];
+#pragma unroll
+          for (int e = 1; e < EPV; e++) m = fmaxf(m, z[e]);
+          if (j >= v1 || m < floor_value) continue;
+#pragma unroll
+          for (int e = 0; e < EPV; e++)
+            if (order_of(z[e]) >= bound) offer(sh, key_of(z[e], head + j * EPV + e));
+        }
       }
     };
     auto largest_below = [&](Key limit) {
@@ -524,7 +534,7 @@ entropy_bwd_kernel(int64_t row0, int vocab, const T* logits, int64_t row_stride,
   for (int e = head + nvec * EPV + part * THREADS + t; e < vocab; e += parts * THREADS) single(e);
 }
 
-// Parts per row: one, unless the row is longer than the block maxima have room for or there are too few rows to fill the chip;
+// Parts per row: one, unless the row is longer than the kept maxima have room for or there are too few rows to fill the chip;
 // then as many as make about 512 workgroups, of at least 512 vectors (two per thread) each.  A part is whole rounds of 256 vectors.
 struct Split { int parts, part_vecs; };
 Split split_rows(int64_t n_rows, int vocab, bool bf16) {
@@ -550,7 +560,7 @@ hipError_t logprob_entropy(int64_t n_rows, int vocab, bool bf16, const void* log
                            hipStream_t st) {
   if (n_rows == 0) return hipSuccess;
   const auto [parts, part_vecs] = split_rows(n_rows, vocab, bf16);
-  const size_t lds = top_k ? ((size_t)part_vecs / THREADS + 1) * THREADS / BLOCK_VECS * sizeof(float) : 0;
+  const size_t lds = top_k ? ((size_t)part_vecs / (ROUNDS * THREADS) + 1) * THREADS * sizeof(float) : 0;
   Partial* partial = (Partial*)workspace;
   Key* keys = (Key*)((char*)workspace + (((size_t)n_rows * parts * sizeof(Partial) + 255) & ~(size_t)255));
   const Outs out{logp, entropy, lse, top_index, top_logp};
