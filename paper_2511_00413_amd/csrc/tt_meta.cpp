@@ -561,7 +561,8 @@ extern "C" tt_status tt_tree_scan_program(int32_t n_chunks, const int32_t* chunk
   // A wave walks a piece token by token, so short pieces are what fills the chip and shortens the walk of a small tree.  Long ones
   // leave fewer end states to be worked out before the outputs can be (the last piece of a branch needs none) and fewer states to
   // walk along the tree.  So: the longest that leave enough waves.  Forward above 64 tokens, enough is what evens out pieces of
-  // unequal length: 16406 tokens of 8192 channels in 148 / 75 / 26 pieces (18944 / 9600 / 3328 waves) 902 / 968 / 1382 us.
+  // unequal length: 16406 tokens of 8192 channels in 269 / 140 / 74 / 40 / 26 pieces (128 waves
+  // each) 876 / 840 / 838 / 896 / 1068 us.
   const int64_t waves = ((int64_t)channels + 63) / 64;
   auto none = [](int64_t, int32_t, int32_t, int32_t, int32_t, int32_t) {};
   int64_t max_tokens = backward ? TT_GDN_CHUNK : TT_SCAN_CHUNK_MAX;

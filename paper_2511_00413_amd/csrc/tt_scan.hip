@@ -63,17 +63,12 @@ scan_carry_kernel(ScanArgs a, int blocks, float* __restrict__ local, float* __re
 
 // One lane per (state, channel) walks the chunk program.  local[chunk] is replaced by the chunk's entering state.
 template <bool LDS>
-__global__ void __launch_bounds__(WALK_THREADS)
+__global__ void __launch_bounds__(WAVE)
 scan_states_kernel(ScanArgs a, float* local, const float* __restrict__ steps, float* saved) {
   extern __shared__ float lds[];
-  const int64_t width = (int64_t)a.n_state * a.channels;
-  if (walk_is_empty(width)) return;
-  const int64_t at = min((int64_t)blockIdx.x * WALK_THREADS + threadIdx.x, width - 1);
-  const int n = (int)(at / a.channels), c = (int)(at - (int64_t)n * a.channels);
-  const int64_t state_at = (int64_t)c * a.n_state + n;
-  const Slots<LDS> slots(lds, saved, width, at);
-  walk_down<LDS>(a, local, steps, width, at, c, a.A[state_at] * LOG2E, a.initial_state ? a.initial_state[state_at] : 0.f, slots,
-                 a.chunk_cap != nullptr, [&](int cap, float s) { a.state_out[cap * width + state_at] = s; });
+  const Walker w(a);
+  walk_down<LDS>(a, local, steps, w, a.A[w.state_at] * LOG2E, Slots<LDS>(a, w, lds, saved), a.chunk_cap != nullptr,
+                 [&](int cap, float s) { a.state_out[cap * w.width + w.state_at] = s; });
 }
 
 template <typename T, int NS, bool GATED>
@@ -129,7 +124,7 @@ size_t up(size_t v) { return (v + 255) & ~(size_t)255; }
 
 size_t scan_fwd_workspace(int channels, int n_state, int n_chunks, int n_slots) {
   const size_t width = (size_t)channels * n_state * sizeof(float);
-  return up(width * n_chunks) + up((size_t)channels * n_chunks * sizeof(float)) + up(width * n_slots) + 256;
+  return up(width * n_chunks) + up((size_t)channels * n_chunks * sizeof(float)) + up(width * (n_slots + EXTRA_SLOTS)) + 256;
 }
 
 hipError_t scan_fwd(const ScanArgs& a, hipStream_t st) {
@@ -150,10 +145,9 @@ hipError_t scan_fwd(const ScanArgs& a, hipStream_t st) {
     if (hipError_t e = hipGetLastError()) return e;
     {
       KernelTimer timer(TT_KERNEL_SCAN_STATES, st);
-      const unsigned walkers = (unsigned)((NS * (int64_t)a.channels + WALK_THREADS - 1) / WALK_THREADS);
-      const size_t lds = (size_t)a.n_slots * WALK_THREADS * sizeof(float);
-      if (a.n_slots <= LDS_SLOTS) scan_states_kernel<true><<<walkers, WALK_THREADS, lds, st>>>(a, local, steps, slots);
-      else scan_states_kernel<false><<<walkers, WALK_THREADS, 0, st>>>(a, local, steps, slots);
+      const unsigned walkers = (unsigned)((NS * (int64_t)a.channels + WAVE - 1) / WAVE);
+      if (a.n_slots <= LDS_SLOTS) scan_states_kernel<true><<<walkers, WAVE, walk_lds(a.n_slots), st>>>(a, local, steps, slots);
+      else scan_states_kernel<false><<<walkers, WAVE, walk_lds(a.n_slots), st>>>(a, local, steps, slots);
     }
     if (hipError_t e = hipGetLastError()) return e;
     KernelTimer timer(TT_KERNEL_SCAN_OUT, st);

@@ -23,7 +23,6 @@ namespace tt {
 namespace {
 using namespace scan;
 
-constexpr int WAVE = 64;
 constexpr int CHUNK = TT_GDN_CHUNK;
 // Tokens whose states are held in registers at a time.  The states in front of them cost 64 bytes of workspace per eight tokens and
 // channel, written once and read once; worked out again from the chunk's start (kept in LDS for every 16 tokens) they were a quarter
@@ -102,64 +101,48 @@ scan_ends_kernel(ScanArgs a, int blocks, float* __restrict__ local, float* __res
 // ---- states --------------------------------------------------------------------------------------
 // local[chunk]: entering state; back[chunk]: gradient of the leaving state.
 template <bool LDS>
-__global__ void __launch_bounds__(WALK_THREADS)
+__global__ void __launch_bounds__(WAVE)
 scan_bwd_states_kernel(ScanArgs a, float* local, float* back, const float* __restrict__ steps, float* saved) {
   extern __shared__ float lds[];
-  const int64_t width = (int64_t)a.n_state * a.channels;
-  if (walk_is_empty(width)) return;
-  const int64_t at = min((int64_t)blockIdx.x * WALK_THREADS + threadIdx.x, width - 1);
-  const int n = (int)(at / a.channels), c = (int)(at - (int64_t)n * a.channels);
-  const int64_t state_at = (int64_t)c * a.n_state + n;
+  const Walker w(a);
   if (a.n_chunks == 0) {
-    if (blockIdx.y) a.d_initial_state[state_at] = 0.f;
+    if (blockIdx.y) a.d_initial_state[w.state_at] = 0.f;
     return;
   }
   // the two walks do not depend on each other: one half of the workgroups takes the way down, the other the way up
-  const Slots<LDS> slots(lds, saved + (blockIdx.y ? a.n_slots * width : 0), width, at);
-  const float a2 = a.A[state_at] * LOG2E;
+  const Slots<LDS> slots(a, w, lds, saved + (blockIdx.y ? (a.n_slots + EXTRA_SLOTS) * w.width : 0));
+  const float a2 = a.A[w.state_at] * LOG2E;
   if (blockIdx.y == 0) {
-    walk_down<LDS>(a, local, steps, width, at, c, a2, a.initial_state ? a.initial_state[state_at] : 0.f, slots, false, [](int, float) {});
+    walk_down<LDS>(a, local, steps, w, a2, slots, false, [](int, float) {});
     return;
   }
   // up the tree: back[chunk] (the gradient of the entering state that the chunk's outputs give) becomes that of the leaving state
-  for (int s = 0; s < a.n_slots; s++) slots[s] = 0.f;                          // gradients of the saved states
-  const bool with_cap = a.d_state_out != nullptr;
-  Program prog;
-  float sent = 0.f, d_first = 0.f, add[2][WALK], len[2][WALK];
-  int nxt_src = -1;                                                            // of the chunk behind
-  const WalkRows rows(a, width, at, c);
-  auto request = [&](int top, float (&r)[WALK], float (&d)[WALK]) { rows.load(back, steps, top - WALK + 1, r, d); };
-  auto walk = [&](int top, const float (&r)[WALK], const float (&d)[WALK]) {
-    float leaving[WALK];
+  for (int s = 0; s <= slots.first; s++) slots[s] = 0.f;                       // gradients of the saved states, and of the first
+  float sent = 0.f;                                                            // by the chunk behind
+  walk<true>(a, back, steps, w, a2, a.d_state_out != nullptr, [&](const Entries& e, const float (&decay)[WALK], const float (&own)[WALK],
+                                                                  float (&leaving)[WALK]) {
+    const uint64_t continued = __ballot(e.src_behind == -2), saves = __ballot(e.dst >= 0), captured = __ballot(e.cap >= 0);
+    const uint64_t used = continued | saves | captured;                        // (steps are not there where no state is used)
+    const uint64_t starts = __ballot(e.src != -2);
+    const int to = e.src < 0 ? slots.first : e.src;
+    float given[WALK];
 #pragma unroll
-    for (int j = 0; j < WALK; j++) {
-      const int u = top - j;
-      if (u >= 0 && u < a.n_chunks) {
-        const int src = Program::at(prog.src, u), dst = Program::at(prog.dst, u), cap = Program::at(prog.cap, u);
-        float g = nxt_src == -2 ? sent : 0.f;
-        bool used = nxt_src == -2;
-        if (dst >= 0) { g += slots[dst]; used = true; }
-        if (cap >= 0) { g += a.d_state_out[cap * width + state_at]; used = true; }
-        leaving[WALK - 1 - j] = g;
-        sent = used ? fmaf(ex2(d[WALK - 1 - j] * a2), g, r[WALK - 1 - j]) : r[WALK - 1 - j];      // (steps are not there where no state is used)
-        if (src == -1) d_first += sent;
-        else if (src >= 0) slots[src] += sent;
-        nxt_src = src;
-      }
+    for (int j = 0; j < WALK; j++) given[j] = 0.f;
+    if (captured)
+#pragma unroll
+      for (int j = 0; j < WALK; j++)
+        if (bit(captured, j)) given[j] = a.d_state_out[Entries::at(e.cap, j) * w.width + w.state_at];
+#pragma unroll
+    for (int j = WALK - 1; j >= 0; j--) {
+      float g = bit(continued, j) ? sent : 0.f;
+      if (bit(saves, j)) g += slots[Entries::at(e.dst, j)];
+      g += given[j];
+      leaving[j] = g;
+      sent = bit(used, j) ? fmaf(decay[j], g, own[j]) : own[j];
+      if (bit(starts, j)) slots[Entries::at(to, j)] += sent;
     }
-    rows.store(back, top - WALK + 1, leaving);
-  };
-  const int last = (a.n_chunks + 2 * WALK - 1) / (2 * WALK) * (2 * WALK) - 1;   // whole rounds: 64 entries at a time line up
-  request(last, add[0], len[0]);
-  prog.load(a, last / 64 * 64, with_cap);
-  for (int top = last; top >= 0; top -= 2 * WALK) {
-    if (top % 64 == 63) prog.load(a, top - 63, with_cap);
-    request(top - WALK, add[1], len[1]);
-    walk(top, add[0], len[0]);
-    if (top - 2 * WALK >= 0) request(top - 2 * WALK, add[0], len[0]);
-    walk(top - WALK, add[1], len[1]);
-  }
-  if (a.d_initial_state) a.d_initial_state[state_at] = d_first;
+  });
+  if (a.d_initial_state) a.d_initial_state[w.state_at] = slots[slots.first];
 }
 
 // ---- grads ---------------------------------------------------------------------------------------
@@ -427,7 +410,7 @@ size_t up(size_t v) { return (v + 255) & ~(size_t)255; }
 
 // Strips of chunks that one wave per channel block takes one after the other, keeping dA in registers: as many as give the chip
 // 6144 waves, three times what it holds at a time (2048 / 4096 / 6144 / 8192 waves and one chunk each, with the sums over the strips,
-// 16406 tokens of 4096 channels: 1031 / 1021 / 1002 / 1016 / 1009 us).
+// 16406 tokens of 4096 channels: 1023 / 1033 / 990 / 1021 / 1005 us).
 int strips_of(int channels, int n_chunks) {
   const int blocks = (channels + WAVE - 1) / WAVE;
   return std::max(1, std::min(n_chunks, (6144 + blocks - 1) / blocks));
@@ -438,7 +421,7 @@ int strips_of(int channels, int n_chunks) {
 size_t scan_bwd_workspace(int64_t n_tokens, int channels, int n_state, int n_chunks, int n_slots) {
   const size_t width = (size_t)channels * n_state * sizeof(float);
   const size_t blocks = (channels + WAVE - 1) / WAVE, strips = strips_of(channels, n_chunks);
-  return 2 * up(width * n_chunks) + up((size_t)channels * n_chunks * sizeof(float)) + up(2 * width * n_slots) +
+  return 2 * up(width * n_chunks) + up((size_t)channels * n_chunks * sizeof(float)) + up(2 * width * (n_slots + EXTRA_SLOTS)) +
          up(width * fronts(n_tokens)) + up((size_t)channels * fronts(n_tokens) * sizeof(float)) +
          up(blocks * n_tokens * 2 * n_state * sizeof(float)) + up(strips * width) + up(strips * 2 * channels * sizeof(float)) + 256;
 }
@@ -451,7 +434,7 @@ hipError_t scan_bwd(const ScanArgs& a, hipStream_t st) {
   float* local = take(width * a.n_chunks);
   float* back = take(width * a.n_chunks);
   float* steps = take((size_t)a.channels * a.n_chunks * sizeof(float));
-  float* slots = take(2 * width * a.n_slots);
+  float* slots = take(2 * width * (a.n_slots + EXTRA_SLOTS));
   float* front_states = take(width * fronts(a.n_tokens));
   float* front_steps = take((size_t)a.channels * fronts(a.n_tokens) * sizeof(float));
   GradBuffers buf{local, back, front_states, front_steps, nullptr, nullptr, nullptr};
@@ -471,10 +454,9 @@ hipError_t scan_bwd(const ScanArgs& a, hipStream_t st) {
     if (hipError_t e = hipGetLastError()) return e;
     if (a.n_chunks > 0 || a.d_initial_state) {
       KernelTimer timer(TT_KERNEL_SCAN_STATES, st);
-      const dim3 walkers((unsigned)((NS * (int64_t)a.channels + WALK_THREADS - 1) / WALK_THREADS), 2);
-      const size_t lds = (size_t)a.n_slots * WALK_THREADS * sizeof(float);
-      if (a.n_slots <= LDS_SLOTS) scan_bwd_states_kernel<true><<<walkers, WALK_THREADS, lds, st>>>(a, local, back, steps, slots);
-      else scan_bwd_states_kernel<false><<<walkers, WALK_THREADS, 0, st>>>(a, local, back, steps, slots);
+      const dim3 walkers((unsigned)((NS * (int64_t)a.channels + WAVE - 1) / WAVE), 2);
+      if (a.n_slots <= LDS_SLOTS) scan_bwd_states_kernel<true><<<walkers, WAVE, walk_lds(a.n_slots), st>>>(a, local, back, steps, slots);
+      else scan_bwd_states_kernel<false><<<walkers, WAVE, walk_lds(a.n_slots), st>>>(a, local, back, steps, slots);
     }
     if (hipError_t e = hipGetLastError()) return e;
     {
