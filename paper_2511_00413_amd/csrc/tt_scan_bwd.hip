@@ -210,6 +210,7 @@ scan_grads_kernel(ScanArgs a, int blocks, int strips, GradBuffers buf) {
   constexpr int SHARE = WAVE / NS, HALF = SHARE / 2;
   struct In { T x, dt, z, dy; };
   __shared__ In inputs[SUB][WAVE];
+  __shared__ float sizes[SUB][WAVE];                                    // the steps' (in registers they would be spilled)
   const int lane = threadIdx.x;
   const int block = blockIdx.x % (unsigned)blocks, strip = blockIdx.x / (unsigned)blocks;
   const int ch = block * WAVE + lane;
@@ -285,15 +286,16 @@ scan_grads_kernel(ScanArgs a, int blocks, int strips, GradBuffers buf) {
 #pragma unroll
         for (int n = 0; n < NS; n++) h0[n] = fmaf(ex2(along * a2[n]), h0[n], from_zero[n]);
       save(before, h0);
-      float h[SUB][NS], delta[SUB];
+      float h[SUB][NS];
       UniformFeed<T, NS> b(a.b, a.b_stride, t0 + base, group * NS), c(a.c, a.c_stride, t0 + base + m - 1, group * NS);
 #pragma unroll
       for (int j = 0; j < SUB; j++) {
         if (j >= m) break;
         Words<T, NS> bv;
         b.next(bv);
-        delta[j] = delta_of(inputs[j][lane].dt);
-        step(j ? h[j - 1] : h0, h[j], bv, delta[j], delta[j] * to_f(inputs[j][lane].x));
+        const float delta = delta_of(inputs[j][lane].dt);
+        sizes[j][lane] = delta;
+        step(j ? h[j - 1] : h0, h[j], bv, delta, delta * to_f(inputs[j][lane].x));
       }
       b.p -= b.step;                             // both from the last token back
       asm volatile("" : "+s"(b.p));              // (the vectors kept from above would be spilled)
@@ -309,12 +311,12 @@ scan_grads_kernel(ScanArgs a, int blocks, int strips, GradBuffers buf) {
         if (j == SUB / 2 - 1 && s && m > SUB / 2) request(s - 1);
         bv = next_b;
         cv = next_c;
+        const In in = inputs[j][lane];
+        const float xv = to_f(in.x), up = to_f(in.dy), delta = sizes[j][lane];
         if (j) {
           b.prev(next_b);
           c.prev(next_c);
         }
-        const In in = inputs[j][lane];
-        const float xv = to_f(in.x), up = to_f(in.dy);
         float g = up, zv = 0.f, sig = 0.f, red[NS];
         if constexpr (GATED) {
           zv = to_f(in.z);
@@ -322,7 +324,7 @@ scan_grads_kernel(ScanArgs a, int blocks, int strips, GradBuffers buf) {
           g *= zv * sig;
         }
         // (a lane past the last channel stands in for it and writes what it writes, but must not be in the sums over the channels)
-        const float u = delta[j] * xv, u_in = valid ? u : 0.f, g_in = valid ? g : 0.f;
+        const float u = delta * xv, u_in = valid ? u : 0.f, g_in = valid ? g : 0.f;
         float y = skip * xv;
 #pragma unroll
         for (int n = 0; n < NS; n++) {
@@ -338,10 +340,10 @@ scan_grads_kernel(ScanArgs a, int blocks, int strips, GradBuffers buf) {
         for (int n = 0; n < NS; n++) {
           red[n] = G[n] * u_in;
           du = fmaf(G[n], bv[n], du);
-          G[n] *= ex2(delta[j] * a2[n]);
+          G[n] *= ex2(delta * a2[n]);
           const float r = G[n] * hp[n];
           dd = fmaf(a2[n], r, dd);
-          dA[n] = fmaf(delta[j], r, dA[n]);
+          dA[n] = fmaf(delta, r, dA[n]);
         }
         const float sum_b = wave_sums<NS>(red, lane);
         bc.so = (base + j) * bc.step;
@@ -353,7 +355,7 @@ scan_grads_kernel(ScanArgs a, int blocks, int strips, GradBuffers buf) {
         dd *= a.use_softplus ? slope : 1.f;
         dbias += dd;
         dx.so = ddt.so = dz.so = (base + j) * dx.step;
-        dx.put(off, fmaf(delta[j], du, skip * g));
+        dx.put(off, fmaf(delta, du, skip * g));
         ddt.put(off, dd);
         if constexpr (GATED) dz.put(off, up * y * sig * (1.f + zv * (1.f - sig)));
       }
