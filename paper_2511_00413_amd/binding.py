@@ -384,16 +384,20 @@ class GdnPlan:
             self.scan_programs[(channels, backward)] = prog
         return prog
 
-    def _scan_chunks(self, channels: int, backward: bool, device, captured: bool):
-        """ctypes tt_scan_chunks of that program on `device`."""
+    def _scan_chunks(self, channels: int, backward: bool, device, captured: bool, stream):
+        """ctypes tt_scan_chunks of that program on `device`, for a call on `stream` (None: the current one)."""
         prog = self._scan_program(channels, backward)
         key = (channels, backward, device)
         on_device = self.scan_programs.get(key)
         if on_device is None:
+            if _torch().cuda.is_current_stream_capturing():
+                raise RuntimeError("the first scan call of a plan with this many channels copies its program: make it before the capture")
             packed = _torch().from_numpy(prog).to(device)
             rows, n = [packed[i].data_ptr() for i in range(5)], prog.shape[1]
             on_device = self.scan_programs[key] = (packed, _ScanChunks(n, self.n_slots, *rows[:4], None),
-                                                   _ScanChunks(n, self.n_slots, *rows))
+                                                   _ScanChunks(n, self.n_slots, *rows), _stream_ptr(None))
+        if _stream_ptr(stream) != on_device[3]:      # not reused, once the plan is dropped, before that stream is through with it
+            on_device[0].record_stream(_torch().cuda.current_stream() if stream is None else stream)
         return on_device[2 if captured else 1]
 
     def _schedule(self):
@@ -1189,8 +1193,9 @@ def tree_scan_fwd(x, dt, A, B, C, plan: GdnPlan, *, D=None, z=None, dt_bias=None
                   return_states: bool = False, out=None, workspace=None, stream=None):
     """Selective state space scan with tree state routing: x, dt [n, channels], B, C [n, groups, states] bf16 or fp32 (free token
     strides), A [channels, states] fp32 (negative), D, dt_bias [channels] fp32 or None, z [n, channels] (the gate) or None; the
-    chunk program is tree_gdn_plan's.  Returns y [n, channels]; with return_states also the end states [n_capture, channels,
-    states] fp32 of the plan's capture nodes.  initial_state [channels, states] fp32: the state every root starts from."""
+    chunk program is tree_gdn_plan's, whose first call with these many channels copies it to the device (so not one that a graph
+    captures).  Returns y [n, channels]; with return_states also the end states [n_capture, channels, states] fp32 of the plan's
+    capture nodes.  initial_state [channels, states] fp32: the state every root starts from."""
     torch = _torch()
     desc = _scan_desc(x, dt, A, B, C, D, z, dt_bias, softplus)
     n, ch, m = desc.n_tokens, desc.channels, desc.n_state
@@ -1202,7 +1207,7 @@ def tree_scan_fwd(x, dt, A, B, C, plan: GdnPlan, *, D=None, z=None, dt_bias=None
     try:
         dev = x.device
         captured = return_states and plan.n_capture > 0
-        chunks = plan._scan_chunks(ch, False, dev, captured)
+        chunks = plan._scan_chunks(ch, False, dev, captured, stream)
         if out is None:
             out = _new((n, ch), x.dtype, dev, stream)
         states = _new((plan.n_capture, ch, m), torch.float32, dev, stream) if return_states else None
@@ -1243,7 +1248,7 @@ def tree_scan_bwd(x, dt, A, B, C, d_y, plan: GdnPlan, *, D=None, z=None, dt_bias
     try:
         dev = x.device
         captured = d_state_out is not None and plan.n_capture > 0
-        chunks = plan._scan_chunks(ch, True, dev, captured)
+        chunks = plan._scan_chunks(ch, True, dev, captured, stream)
         like = lambda t: None if t is None else _new(t.shape, t.dtype, dev, stream)      # noqa: E731
         grads = ScanGrads(like(x), like(x), like(A), like(B), like(C), like(D), like(z), like(dt_bias), like(A) if want_d_initial_state else None)
         need = int(_lib().tt_tree_scan_bwd_workspace(ctypes.byref(desc), chunks.n_chunks, chunks.n_slots))

@@ -644,6 +644,15 @@ bool meets(const Rows& a, const Rows& b) {
   return shares_memory(a.p, a.step * a.es, a.len * a.es, b.p, b.step * b.es, b.len * b.es, a.n);
 }
 
+// Whether one of the outputs (y in rows, a state) lies on an input or on the other.
+bool outputs_meet(const Rows& y, const Span& state, std::initializer_list<Rows> rows, std::initializer_list<Span> whole) {
+  for (const Rows& in : rows)
+    if (meets(y, in) || meets(state, in.span())) return true;
+  for (const Span& in : whole)
+    if (meets(y.span(), in) || meets(state, in)) return true;
+  return meets(y.span(), state);
+}
+
 bool aligned_to(const void* p, size_t n) { return reinterpret_cast<uintptr_t>(p) % n == 0; }
 
 // Sizes and strides of a scan descriptor; strides of 0 are filled in.
@@ -744,11 +753,11 @@ extern "C" tt_status tt_tree_scan_fwd(const tt_scan_desc* desc, const tt_scan_ch
   if (!aligned_to(y, es)) return fail(TT_ERR_ALIGN, "y is not aligned to its element size");
   if (!tt::aligned16(initial_state) || !tt::aligned16(state_out)) return fail(TT_ERR_ALIGN, "a state is not 16-byte aligned");
   const int64_t bc = (int64_t)d.groups * d.n_state;
-  const Rows out{y, n, d.channels, d.y_stride_tok, es};
-  for (const Rows& in : {Rows{x, n, d.channels, d.x_stride_tok, es}, Rows{dt, n, d.channels, d.dt_stride_tok, es},
-                         Rows{z, n, d.channels, d.z_stride_tok, es}, Rows{b, n, bc, d.b_stride_tok, es}, Rows{c, n, bc, d.c_stride_tok, es}})
-    if (meets(out, in)) return fail(TT_ERR_SHAPE, "y shares memory with an input");
-  if (meets(Span{state_out, state_out ? width : 0}, Span{initial_state, width})) return fail(TT_ERR_SHAPE, "state_out shares memory with initial_state");
+  if (outputs_meet({y, n, d.channels, d.y_stride_tok, es}, {state_out, state_out ? width : 0},
+                   {{x, n, d.channels, d.x_stride_tok, es}, {dt, n, d.channels, d.dt_stride_tok, es}, {z, n, d.channels, d.z_stride_tok, es},
+                    {b, n, bc, d.b_stride_tok, es}, {c, n, bc, d.c_stride_tok, es}},
+                   {{A, width}, {D, d.channels * 4}, {dt_bias, d.channels * 4}, {initial_state, width}}))
+    return fail(TT_ERR_SHAPE, "an output shares memory with another tensor");
   const size_t need = tt::scan_fwd_workspace(d.channels, d.n_state, chunks->n_chunks, chunks->n_slots);
   if (!workspace || workspace_bytes < need || !tt::aligned16(workspace))
     return fail(TT_ERR_WORKSPACE, "scan forward needs %zu bytes of 16-byte aligned workspace, got %zu", need, workspace_bytes);
@@ -813,10 +822,12 @@ extern "C" tt_status tt_tree_scan_step(const tt_scan_desc* desc, const void* x, 
   if (!tt::aligned16(state) || !tt::aligned16(state_out)) return fail(TT_ERR_ALIGN, "a state is not 16-byte aligned");
   if (!(state_out == state && !index) && meets(Span{state_out, n * width * 4}, Span{state, n_slots * width * 4}))
     return fail(TT_ERR_SHAPE, "state_out may share memory with state only as a whole and without an index");
-  const Rows out{y, n, d.channels, d.y_stride_tok, es};
-  for (const Rows& in : {Rows{x, n, d.channels, d.x_stride_tok, es}, Rows{dt, n, d.channels, d.dt_stride_tok, es},
-                         Rows{z, n, d.channels, d.z_stride_tok, es}, Rows{b, n, bc, d.b_stride_tok, es}, Rows{c, n, bc, d.c_stride_tok, es}})
-    if (meets(out, in)) return fail(TT_ERR_SHAPE, "y shares memory with an input");
+  if (outputs_meet({y, n, d.channels, d.y_stride_tok, es}, {state_out, n * width * 4},
+                   {{x, n, d.channels, d.x_stride_tok, es}, {dt, n, d.channels, d.dt_stride_tok, es}, {z, n, d.channels, d.z_stride_tok, es},
+                    {b, n, bc, d.b_stride_tok, es}, {c, n, bc, d.c_stride_tok, es}},
+                   {{A, width * 4}, {D, d.channels * 4}, {dt_bias, d.channels * 4}, {index, n * 4}}) ||
+      meets(Rows{y, n, d.channels, d.y_stride_tok, es}.span(), Span{state, n_slots * width * 4}))
+    return fail(TT_ERR_SHAPE, "an output shares memory with another tensor");
   tt::ScanStepArgs a{};
   a.n_rows = (int)n; a.channels = d.channels; a.n_state = d.n_state; a.groups = d.groups; a.n_slots = n_slots; a.use_softplus = d.softplus == 1;
   a.x = x; a.dt = dt; a.z = z; a.b = b; a.c = c; a.A = A; a.D = D; a.dt_bias = dt_bias; a.state = state; a.index = index;

@@ -412,7 +412,7 @@ size_t up(size_t v) { return (v + 255) & ~(size_t)255; }
 
 // Strips of chunks that one wave per channel block takes one after the other, keeping dA in registers: as many as give the chip
 // 6144 waves, three times what it holds at a time (2048 / 4096 / 6144 / 8192 waves and one chunk each, with the sums over the strips,
-// 16406 tokens of 4096 channels: 1023 / 1033 / 990 / 1021 / 1005 us).
+// 16406 tokens of 4096 channels: 1014 / 1004 / 946 / 998 / 983 us).
 int strips_of(int channels, int n_chunks) {
   const int blocks = (channels + WAVE - 1) / WAVE;
   return std::max(1, std::min(n_chunks, (6144 + blocks - 1) / blocks));

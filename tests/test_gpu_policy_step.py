@@ -240,3 +240,39 @@ def test_a_given_stream_while_another_is_current():
     torch.cuda.synchronize()
     for i, (a, b) in enumerate(zip(got, want)):
         assert torch.equal(a, b), i
+
+
+def scan_inputs(n=300, channels=256):
+    g = torch.Generator(device="cuda").manual_seed(8)
+    f = lambda *s: torch.randn(s, generator=g, device="cuda")          # noqa: E731
+    return f(n, channels), f(n, channels), -f(channels, 8).abs(), f(n, 1, 8), f(n, 1, 8)
+
+
+def test_a_plan_dropped_behind_its_call():
+    """The plan's device copy stays until the stream that a call was given is through with it."""
+    ins, tree = scan_inputs(), ([-1, 0, 0, 1, 1], [60] * 5)
+    want = T.tree_scan_fwd(*ins, T.tree_gdn_plan(*tree))
+    busy = torch.randn(4096, 4096, device="cuda")
+    other = torch.cuda.Stream()
+    other.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(other):
+        for _ in range(8):
+            busy = busy @ busy * 1e-2
+    T.tree_scan_fwd(*ins, plan := T.tree_gdn_plan(*tree))               # the copy is made on the current stream
+    pieces = plan._scan_program(256, False).size
+    got = T.tree_scan_fwd(*ins, plan, stream=other)
+    del plan
+    for _ in range(20):                                                 # the current stream takes and clears memory of that size
+        torch.zeros(pieces, dtype=torch.int32, device="cuda")
+    torch.cuda.synchronize()
+    assert torch.equal(got, want)
+
+
+def test_a_first_scan_call_is_not_captured():
+    ins, tree = scan_inputs(), ([-1, 0], [200, 100])
+    plan, want = T.tree_gdn_plan(*tree), T.tree_scan_fwd(*ins, T.tree_gdn_plan(*tree))
+    torch.cuda.synchronize()
+    with pytest.raises(RuntimeError, match="before the capture"):
+        with torch.cuda.graph(torch.cuda.CUDAGraph()):
+            T.tree_scan_fwd(*ins, plan)
+    assert torch.equal(T.tree_scan_fwd(*ins, plan), want)

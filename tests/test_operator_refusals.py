@@ -120,6 +120,25 @@ def test_steps():
         assert call(**a) == code and T.last_error(), a
 
 
+def test_scan_outputs_on_other_tensors():
+    f = L.tt_tree_scan_fwd
+    ok = dict(x=FAKE[0], dt=FAKE[1], A=FAKE[2], b=FAKE[3], c=FAKE[4], D=FAKE[5], z=FAKE[6], bias=FAKE[7], init=FAKE[8], so=FAKE[11], y=FAKE[9],
+              ws=FAKE[10], wb=BIG)
+    call = lambda **a: f(ctypes.byref(scan_desc()), ctypes.byref(chunks(cap=FAKE[0])), *{**ok, **a}.values(), None)      # noqa: E731
+    for i in (2, 5, 7, 8, 11):
+        assert call(y=FAKE[i]) == -2 and T.last_error(), i
+    for i in range(10):
+        assert call(so=FAKE[i]) == -2 and T.last_error(), i
+    f = L.tt_tree_scan_step
+    ok = dict(x=FAKE[0], dt=FAKE[1], A=FAKE[2], b=FAKE[3], c=FAKE[4], D=FAKE[5], z=FAKE[6], bias=FAKE[7], slots=100, s=FAKE[8], i=FAKE[9],
+              so=FAKE[10], y=FAKE[11])
+    call = lambda **a: f(ctypes.byref(scan_desc()), *{**ok, **a}.values(), None)                                          # noqa: E731
+    for i in range(11):
+        assert call(y=FAKE[i]) == -2 and T.last_error(), i
+        if i < 10:
+            assert call(so=FAKE[i]) == -2 and T.last_error(), i
+
+
 def test_binding():
     z, y = torch.zeros(4, 50), torch.zeros(4, dtype=torch.int32)
     f32 = lambda *s: torch.zeros(s)                                           # noqa: E731
