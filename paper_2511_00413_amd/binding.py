@@ -609,6 +609,8 @@ def _check_rows(t, name, shape, dtypes):
     """Rows of contiguous elements with a free stride between them (one of the dtypes); returns that stride in elements."""
     if t.shape != shape or t.dtype not in dtypes:
         raise ValueError(f"{name} must be {shape} of {' / '.join(str(d) for d in dtypes)}")
+    if t.is_contiguous():
+        return shape[1] if len(shape) == 2 else shape[1] * shape[2]
     step = t.stride()
     row = 1
     for i in range(len(shape) - 1, 0, -1):
@@ -638,9 +640,15 @@ def _enter_device(*tensors):
     return before
 
 
-def _new(shape, dtype, device, stream):
-    """An empty tensor for a call on `stream` (None: the current one): not reused, once dropped, before that stream is through."""
-    t = _TORCH.empty(shape, dtype=dtype, device=device)
+def _new(like, shape, stream, dtype=None):
+    """An empty tensor on the device of `like` (and of its dtype) for a call on `stream` (None: the current one): not reused, once
+    dropped, before that stream is through."""
+    if dtype is not None:
+        t = like.new_empty(shape, dtype=dtype)
+    elif like.shape == shape and like.is_contiguous():
+        t = _TORCH.empty_like(like)                       # the quickest of the three
+    else:
+        t = like.new_empty(shape)
     if stream is not None:
         t.record_stream(stream)
     return t
@@ -772,7 +780,7 @@ def tree_rope_axes(x, axis_pos, sections, *, interleaved: bool = False, theta_ba
     before = _enter_device(x, axis_pos, out)
     try:
         if out is None:
-            out = _new((n, h, d), x.dtype, x.device, stream)
+            out = _new(x, (n, h, d), stream)
         _check(_lib().tt_tree_rope_axes(n, h, d, DTYPE_BF16 if x.dtype == torch.bfloat16 else DTYPE_FP32, _dp(x), stride, n_axes,
                                         _dp(axis_pos), pair_axis, float(theta_base), 1 if inverse else 0, _dp(out), out_stride,
                                         _stream_ptr(stream)))
@@ -841,14 +849,14 @@ def tree_logprob_entropy(logits, target, *, top_k: int = 0, logp=None, entropy=N
         _check_tensor(top_logp, "top_logp", (n, top_k), torch.float32)
     before = _enter_device(logits, target, logp, entropy, lse, top_index, top_logp, workspace)
     try:
-        dev = logits.device
-        new = lambda *shape, dtype=torch.float32: _new(shape, dtype, dev, stream)      # noqa: E731
-        logp, entropy, lse = (new(n) if t is None else t for t in (logp, entropy, lse))
+        logp = _new(logits, (n,), stream, torch.float32) if logp is None else logp
+        entropy = _new(logp, (n,), stream) if entropy is None else entropy
+        lse = _new(logp, (n,), stream) if lse is None else lse
         if top_k:
-            top_index = new(n, top_k, dtype=torch.int32) if top_index is None else top_index
-            top_logp = new(n, top_k) if top_logp is None else top_logp
+            top_logp = _new(logp, (n, top_k), stream) if top_logp is None else top_logp
+            top_index = _new(top_logp, (n, top_k), stream, torch.int32) if top_index is None else top_index
         if workspace is None:
-            workspace = new(need, dtype=torch.uint8)
+            workspace = _new(logits, (need,), stream, torch.uint8)
         _check(_lib().tt_tree_logprob_entropy(n, vocab, code, _dp(logits), stride, _dp(target), top_k, _dp(logp), _dp(entropy),
                                               _dp(lse), _dp(top_index), _dp(top_logp), _dp(workspace),
                                               workspace.numel() * workspace.element_size(), _stream_ptr(stream)))
@@ -876,7 +884,7 @@ def tree_logprob_entropy_bwd(logits, target, lse, entropy, d_logp=None, d_entrop
     before = _enter_device(logits, target, lse, entropy, d_logp, d_entropy, out)
     try:
         if out is None:
-            out = _new((n, vocab), logits.dtype, logits.device, stream)
+            out = _new(logits, (n, vocab), stream)
         _check(_lib().tt_tree_logprob_entropy_bwd(n, vocab, code, _dp(logits), stride, _dp(target), _dp(lse), _dp(entropy),
                                                   _dp(d_logp), _dp(d_entropy), _dp(out), out_stride, _stream_ptr(stream)))
     finally:
@@ -1209,11 +1217,11 @@ def tree_scan_fwd(x, dt, A, B, C, plan: GdnPlan, *, D=None, z=None, dt_bias=None
         captured = return_states and plan.n_capture > 0
         chunks = plan._scan_chunks(ch, False, dev, captured, stream)
         if out is None:
-            out = _new((n, ch), x.dtype, dev, stream)
-        states = _new((plan.n_capture, ch, m), torch.float32, dev, stream) if return_states else None
+            out = _new(x, (n, ch), stream)
+        states = _new(A, (plan.n_capture, ch, m), stream) if return_states else None
         need = int(_lib().tt_tree_scan_fwd_workspace(ctypes.byref(desc), chunks.n_chunks, chunks.n_slots))
         if workspace is None:
-            workspace = _new(max(need, 256), torch.uint8, dev, stream)
+            workspace = _new(x, (max(need, 256),), stream, torch.uint8)
         _check(_lib().tt_tree_scan_fwd(ctypes.byref(desc), ctypes.byref(chunks), _dp(x), _dp(dt), _dp(A), _dp(B), _dp(C), _dp(D), _dp(z),
                                        _dp(dt_bias), _dp(initial_state), _dp(states) if captured else None, _dp(out), _dp(workspace),
                                        workspace.numel() * workspace.element_size(), _stream_ptr(stream)))
@@ -1249,11 +1257,11 @@ def tree_scan_bwd(x, dt, A, B, C, d_y, plan: GdnPlan, *, D=None, z=None, dt_bias
         dev = x.device
         captured = d_state_out is not None and plan.n_capture > 0
         chunks = plan._scan_chunks(ch, True, dev, captured, stream)
-        like = lambda t: None if t is None else _new(t.shape, t.dtype, dev, stream)      # noqa: E731
+        like = lambda t: None if t is None else _new(t, t.shape, stream)      # noqa: E731
         grads = ScanGrads(like(x), like(x), like(A), like(B), like(C), like(D), like(z), like(dt_bias), like(A) if want_d_initial_state else None)
         need = int(_lib().tt_tree_scan_bwd_workspace(ctypes.byref(desc), chunks.n_chunks, chunks.n_slots))
         if workspace is None:
-            workspace = _new(max(need, 256), torch.uint8, dev, stream)
+            workspace = _new(x, (max(need, 256),), stream, torch.uint8)
         _check(_lib().tt_tree_scan_bwd(ctypes.byref(desc), ctypes.byref(chunks), _dp(x), _dp(dt), _dp(A), _dp(B), _dp(C), _dp(D), _dp(z),
                                        _dp(dt_bias), _dp(initial_state), _dp(d_y), _dp(d_state_out) if captured else None,
                                        *(_dp(g) for g in grads), _dp(workspace), workspace.numel() * workspace.element_size(),
@@ -1282,9 +1290,9 @@ def tree_scan_step(x, dt, A, B, C, state, *, index=None, D=None, z=None, dt_bias
     before = _enter_device(x, dt, A, B, C, D, z, dt_bias, state, index, state_out, out)
     try:
         if out is None:
-            out = _new((n, ch), x.dtype, x.device, stream)
+            out = _new(x, (n, ch), stream)
         if state_out is None:
-            state_out = _new((n, ch, m), torch.float32, x.device, stream)
+            state_out = _new(state, (n, ch, m), stream)
         _check(_lib().tt_tree_scan_step(ctypes.byref(desc), _dp(x), _dp(dt), _dp(A), _dp(B), _dp(C), _dp(D), _dp(z), _dp(dt_bias), slots,
                                         _dp(state), _dp(index), _dp(state_out), _dp(out), _stream_ptr(stream)))
     finally:
@@ -1315,9 +1323,9 @@ def tree_conv_step(x, state, weight, bias=None, *, index=None, silu: bool = True
     before = _enter_device(x, state, weight, bias, index, state_out, out)
     try:
         if out is None:
-            out = _new((n, c), x.dtype, x.device, stream)
+            out = _new(x, (n, c), stream)
         if state_out is None:
-            state_out = _new((n, k - 1, c), x.dtype, x.device, stream)
+            state_out = _new(state, (n, k - 1, c), stream)
         _check(_lib().tt_tree_conv_step(n, c, k, DTYPE_BF16 if x.dtype == torch.bfloat16 else DTYPE_FP32, 1 if silu else 0, _dp(x), xs,
                                         _dp(weight), _dp(bias), slots, _dp(state), _dp(index), _dp(state_out), _dp(out), ys,
                                         _stream_ptr(stream)))
