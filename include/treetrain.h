@@ -728,6 +728,8 @@ typedef struct {
 typedef struct {
   int32_t n_chunks, n_slots;
   const int32_t *chunk_tok0, *chunk_len, *chunk_src, *chunk_dst, *chunk_cap;      /* device */
+  const int32_t* chunk_order;       /* device; NULL, or a permutation of the chunks: the order in which they are
+                                       started (the longest first, and the last to end are short)             */
 } tt_scan_chunks;
 tt_status tt_tree_scan_program(int32_t n_chunks, const int32_t* chunk_tok0, const int32_t* chunk_len,
                                const int32_t* chunk_src, const int32_t* chunk_dst, const int32_t* chunk_cap,

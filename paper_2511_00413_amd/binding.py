@@ -319,7 +319,7 @@ class _ScanDesc(ctypes.Structure):
 
 class _ScanChunks(ctypes.Structure):
     _fields_ = [("n_chunks", ctypes.c_int32), ("n_slots", ctypes.c_int32)] + \
-               [(name, _vp) for name in ("chunk_tok0", "chunk_len", "chunk_src", "chunk_dst", "chunk_cap")]
+               [(name, _vp) for name in ("chunk_tok0", "chunk_len", "chunk_src", "chunk_dst", "chunk_cap", "chunk_order")]
 
 
 class _GdnSchedule(ctypes.Structure):
@@ -392,9 +392,10 @@ class GdnPlan:
         if on_device is None:
             if _torch().cuda.is_current_stream_capturing():
                 raise RuntimeError("the first scan call of a plan with this many channels copies its program: make it before the capture")
-            packed = _torch().from_numpy(prog).to(device)
-            rows, n = [packed[i].data_ptr() for i in range(5)], prog.shape[1]
-            on_device = self.scan_programs[key] = (packed, _ScanChunks(n, self.n_slots, *rows[:4], None),
+            longest_first = np.argsort(-prog[1], kind="stable").astype(np.int32)      # (the last to end are short)
+            packed = _torch().from_numpy(np.concatenate([prog, longest_first[None]])).to(device)
+            rows, n = [packed[i].data_ptr() for i in range(6)], prog.shape[1]
+            on_device = self.scan_programs[key] = (packed, _ScanChunks(n, self.n_slots, *rows[:4], None, rows[5]),
                                                    _ScanChunks(n, self.n_slots, *rows), _stream_ptr(None))
         if _stream_ptr(stream) != on_device[3]:      # not reused, once the plan is dropped, before that stream is through with it
             on_device[0].record_stream(_torch().cuda.current_stream() if stream is None else stream)

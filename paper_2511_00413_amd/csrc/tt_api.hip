@@ -719,6 +719,7 @@ tt::ScanArgs scan_args(const tt_scan_desc& d, const tt_scan_chunks& k) {
   a.x_stride = d.x_stride_tok; a.dt_stride = d.dt_stride_tok; a.z_stride = d.z_stride_tok; a.b_stride = d.b_stride_tok;
   a.c_stride = d.c_stride_tok; a.y_stride = a.dy_stride = d.y_stride_tok;
   a.chunk_tok0 = k.chunk_tok0; a.chunk_len = k.chunk_len; a.chunk_src = k.chunk_src; a.chunk_dst = k.chunk_dst; a.chunk_cap = k.chunk_cap;
+  a.chunk_order = k.chunk_order;
   return a;
 }
 

@@ -166,7 +166,7 @@ struct ScanArgs {
   const void *x, *dt, *z, *b, *c, *dy;            // z: nullptr = no gate; dy: backward only
   int64_t x_stride, dt_stride, z_stride, b_stride, c_stride, dy_stride;
   const float *A, *D, *dt_bias;                   // [channels][n_state], [channels] or nullptr
-  const int32_t *chunk_tok0, *chunk_len, *chunk_src, *chunk_dst, *chunk_cap;
+  const int32_t *chunk_tok0, *chunk_len, *chunk_src, *chunk_dst, *chunk_cap, *chunk_order;
   const float* initial_state;                     // [channels][n_state] or nullptr
   void* y;                                        // forward
   int64_t y_stride;

@@ -521,21 +521,24 @@ extern "C" tt_status tt_tree_gdn_plan(int32_t n_nodes, const int32_t* parent, co
 
 namespace {
 // Every maximal run of chunks whose state stays on chip, in as few pieces of at most max_tokens as that needs, of about equal length
-// (whole groups of eight tokens).
+// (whole groups of eight tokens); of a run that nothing goes on from, the last up to `tail` tokens in one piece.
 template <typename Emit>
 int64_t cut_runs(int32_t n_chunks, const int32_t* tok0, const int32_t* len, const int32_t* src, const int32_t* dst, const int32_t* cap,
-                 int64_t max_tokens, Emit emit) {
+                 int64_t max_tokens, int64_t tail, Emit emit) {
   int64_t n = 0;
   for (int32_t c = 0; c < n_chunks;) {
     int32_t end = c + 1;
     int64_t total = len[c];
     while (end < n_chunks && src[end] == -2 && dst[end - 1] < 0 && (!cap || cap[end - 1] < 0)) total += len[end++];
-    const int64_t parts = (total + max_tokens - 1) / max_tokens;
-    const int64_t piece = ((total + parts - 1) / parts + 7) / 8 * 8;
-    for (int64_t at = 0; at < total; at += piece, n++) {
-      const bool last = at + piece >= total;
-      emit(n, (int32_t)(tok0[c] + at), (int32_t)(last ? total - at : piece), at ? -2 : src[c], last ? dst[end - 1] : -1,
-           last && cap ? cap[end - 1] : -1);
+    const bool used = dst[end - 1] >= 0 || (cap && cap[end - 1] >= 0) || (end < n_chunks && src[end] == -2);
+    const int64_t front = used ? total : std::max(total - tail, (int64_t)0);       // (what goes in short pieces)
+    const int64_t parts = (front + max_tokens - 1) / max_tokens;
+    const int64_t piece = parts ? ((front + parts - 1) / parts + 7) / 8 * 8 : total;
+    for (int64_t at = 0, k = 0; at < total; n++, k++) {
+      const bool last = used ? at + piece >= total : k == parts;
+      const int64_t size = last ? total - at : piece;
+      emit(n, (int32_t)(tok0[c] + at), (int32_t)size, at ? -2 : src[c], last ? dst[end - 1] : -1, last && cap ? cap[end - 1] : -1);
+      at += size;
     }
     c = end;
   }
@@ -558,23 +561,31 @@ extern "C" tt_status tt_tree_scan_program(int32_t n_chunks, const int32_t* chunk
     if (chunk_src[c] == -2 && (c == 0 || chunk_tok0[c] != chunk_tok0[c - 1] + chunk_len[c - 1]))
       return tt::fail(TT_ERR_TREE, "chunk %d continues no chunk", c);
   }
-  // A wave walks a piece token by token, so short pieces are what fills the chip and shortens the walk of a small tree.  Long ones
-  // leave fewer end states to be worked out before the outputs can be (the last piece of a branch needs none) and fewer states to
-  // walk along the tree.  So: the longest that leave enough waves.  Forward above 64 tokens, enough is what evens out pieces of
-  // unequal length: 16406 tokens of 8192 channels in 269 / 140 / 74 / 40 / 26 pieces (128 waves
-  // each) 876 / 840 / 838 / 896 / 1068 us.
-  const int64_t waves = ((int64_t)channels + 63) / 64;
-  auto none = [](int64_t, int32_t, int32_t, int32_t, int32_t, int32_t) {};
-  int64_t max_tokens = backward ? TT_GDN_CHUNK : TT_SCAN_CHUNK_MAX;
-  for (; max_tokens > 16; max_tokens /= 2)
-    if (waves * cut_runs(n_chunks, chunk_tok0, chunk_len, chunk_src, chunk_dst, chunk_cap, max_tokens, none) >=
-        (max_tokens > TT_GDN_CHUNK ? 12288 : 4096))
-      break;
-  const int64_t n = cut_runs(n_chunks, chunk_tok0, chunk_len, chunk_src, chunk_dst, chunk_cap, max_tokens, none);
+  // A wave walks a piece token by token, so short pieces fill the chip and shorten the walk of a small tree, and long ones leave fewer
+  // states to be walked along the tree.  `share` is what a SIMD has to do in all, in tokens of 64 channels: a piece takes part of it.
+  // Forward the last piece of a branch that nothing goes on from is longer than the others where there is room, as its tokens are
+  // worked on once (every other piece twice: its end state before the outputs): up to two fifths of the share, the others up to a
+  // quarter of that, but 64.  16 states, us: 16406 tokens of 8192 channels (share 2051) in pieces to 128 730, the last to 256 674, to
+  // 512 634, to 256 and 1024 815; 16384 tokens of 4096 channels in a chain (1024) 64 / 256 403, 128 / 512 508, all 64 413; 3000 tokens of
+  // 4096 channels (187) 64 / 64 90, 64 / 128 103, 32 / 32 102; 2111 tokens of 2048 channels (66) 16 / 16 63, 32 / 32 58, 64 / 64 73.
+  // Backward all pieces are worked on twice: 16406 tokens of 4096 channels (1025) 64 1247, 32 1326; 8000 tokens of 2048 channels (250) 64
+  // 386, 32 373, 16 413; 6000 tokens of 1024 channels in a chain (94) 64 132, 32 120, 16 142; 777 tokens of 1024 (12) 32 83, 16 62.
+  int64_t tokens = 0;
+  for (int32_t c = 0; c < n_chunks; c++) tokens += chunk_len[c];
+  const int64_t share = tokens * (((int64_t)channels + 63) / 64) / 1024;
+  int64_t tail = TT_SCAN_CHUNK_MAX, max_tokens = share >= 400 ? 64 : share >= 80 ? 32 : 16;
+  if (backward) {
+    tail = max_tokens;
+  } else {
+    while (tail > 16 && 5 * tail > 2 * share) tail /= 2;
+    max_tokens = std::min(tail, std::max(tail / 4, (int64_t)64));
+  }
+  const int64_t n = cut_runs(n_chunks, chunk_tok0, chunk_len, chunk_src, chunk_dst, chunk_cap, max_tokens, tail,
+                             [](int64_t, int32_t, int32_t, int32_t, int32_t, int32_t) {});
   if (n > INT32_MAX) return tt::fail(TT_ERR_SHAPE, "more than 2^31 - 1 pieces");
   *n_pieces = (int32_t)n;
   if (!count_only)
-    cut_runs(n_chunks, chunk_tok0, chunk_len, chunk_src, chunk_dst, chunk_cap, max_tokens,
+    cut_runs(n_chunks, chunk_tok0, chunk_len, chunk_src, chunk_dst, chunk_cap, max_tokens, tail,
              [&](int64_t i, int32_t t0, int32_t n_tok, int32_t from, int32_t to, int32_t captured) {
                tok0[i] = t0; len[i] = n_tok; src[i] = from; dst[i] = to;
                if (cap) cap[i] = captured;

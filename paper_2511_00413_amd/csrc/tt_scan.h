@@ -70,7 +70,8 @@ constexpr int AHEAD = 4;                   // tokens whose loads are in flight b
 struct Place { int chunk, c; bool valid; int64_t cc; int group; };
 __device__ __forceinline__ Place place(const ScanArgs& a, int blocks) {
   Place p;
-  p.chunk = blockIdx.x / (unsigned)blocks;
+  p.chunk = (int)(blockIdx.x / (unsigned)blocks);
+  if (a.chunk_order) p.chunk = a.chunk_order[p.chunk];
   p.c = (int)(blockIdx.x % (unsigned)blocks) * THREADS + threadIdx.x;
   p.valid = p.c < a.channels;
   p.cc = p.valid ? p.c : a.channels - 1;

@@ -272,3 +272,16 @@ def test_given_workspaces_are_not_overrun():
         with pytest.raises(T.TreeTrainError):
             call(ws[:need - 1])
     torch.cuda.synchronize()
+
+
+def test_order_of_the_pieces():
+    """Pieces are independent: started in another order they give the same bits."""
+    tree = W.random_tree(21, n_nodes=14, lo=30, hi=400)
+    plan = T.tree_gdn_plan(tree.parent, tree.seg_len)
+    k = cuda(make(int(tree.seg_len.sum()), 320, 16, 1, torch.bfloat16, 3))
+    run = lambda: T.tree_scan_fwd(k["x"], k["dt"], k["A"], k["B"], k["C"], plan, D=k["D"], z=k["z"], dt_bias=k["dt_bias"])    # noqa: E731
+    want = run()
+    held = next(v for key, v in plan.scan_programs.items() if len(key) == 3)
+    for order in (None, torch.arange(held[1].n_chunks - 1, -1, -1, dtype=torch.int32, device="cuda")):
+        held[1].chunk_order = None if order is None else order.data_ptr()
+        assert torch.equal(run(), want)

@@ -34,9 +34,16 @@ def test_program(seed, lo, hi, channels, backward):
     out = plan._scan_program(channels, backward).tolist()
     arrays = [plan.chunk_tok0, plan.chunk_len, plan.chunk_src, plan.chunk_dst, plan.chunk_cap]
     assert ends(*out, plan.n_slots) == ends(*(a.tolist() for a in arrays), plan.n_slots)
-    assert max(out[1]) <= (64 if backward else 1024) and min(out[1]) >= 1
-    waves = len(out[0]) * -(-channels // 64)
-    assert max(out[1]) <= 16 or waves >= (12288 if max(out[1]) > 64 else 4096)
+    assert min(out[1]) >= 1
+    share = sum(out[1]) * -(-channels // 64) // 1024
+    if backward:
+        most = tail = 64 if share >= 400 else 32 if share >= 80 else 16
+    else:
+        tail = max(t for t in (16, 32, 64, 128, 256, 512, 1024) if t == 16 or 5 * t <= 2 * share)
+        most = min(tail, max(tail // 4, 64))
+    for i, n in enumerate(out[1]):
+        goes_on = out[3][i] >= 0 or out[4][i] >= 0 or (i + 1 < len(out[1]) and out[2][i + 1] == -2)
+        assert n <= (most if goes_on else tail), i
 
 
 def test_empty_and_refusals():
