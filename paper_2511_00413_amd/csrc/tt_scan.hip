@@ -7,12 +7,12 @@
 //   carry   every chunk that something goes on from: the state it would leave from zero, and the sum of its steps (the decay over
 //           the chunk is exp(A sum delta), one exponential)
 //   states  down the tree, one lane per (channel, state): entering state of every chunk
-//   out     every chunk again from its entering state, with the outputs
+//   out     every chunk again from its entering state, with the outputs; the longest first, if the caller says which
 // One lane holds one channel with all its states in registers; B and C are the same for a wave's 64 channels and come as scalar
 // operands.  Nothing is shared between lanes, and everything is fp32 until the output is rounded.
 //
 // Bound by the vector ALU: 16 states cost an exponential (two issue slots) and four to five plain instructions each, against 8
-// bytes of bf16 per token and channel.
+// bytes of bf16 per token and channel.  16406 tokens of 8192 channels: carry 207 us over 58 % of the tokens, states 26, out 446.
 #include <algorithm>
 #include "tt_scan.h"
 
