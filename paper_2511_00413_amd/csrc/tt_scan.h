@@ -146,10 +146,12 @@ __device__ __forceinline__ void stream(int len, Request request, Work work) {
 // on the walk, so the rows of WALK chunks are requested before the WALK in front of them are walked.  A walk is one chain of dependent
 // steps, and on a small tree most entries begin or end a branch: no step down branches on its entry, and a saved state is read two
 // entries before it is used (down 78 entries of 1024 channels and 16 states, 54 of which start from a saved state: 18.3 us with
-// branches and reads on the spot, 15.1 so, 10.6 without any step; 269 entries of 4096 channels, down and up: 73 and 67, 58 of them
-// the bytes).
+// branches and reads on the spot, 14 so; 143 entries of 2048 channels, down and up: 35 and 25; 269 of 4096 channels: 73 and 66, 58 of
+// them the bytes).
 constexpr int WALK = 16;
 constexpr int WAVE = 64;
+// Rows of the arrays that are walked: WALK are read and written at a time, and nothing comes of those past the end.
+inline size_t walk_rows(int n_chunks) { return (size_t)n_chunks + WALK - 1; }
 constexpr int LDS_SLOTS = 64;                   // saved states held in LDS: up to 16 KB a workgroup; more live in the workspace
 // Two more than the program has: FIRST, for what a root starts from, and one for what is written and never read.
 constexpr int EXTRA_SLOTS = 2;
@@ -196,7 +198,8 @@ struct Entries {
   }
   static __device__ __forceinline__ int at(int v, int j) { return __builtin_amdgcn_readlane(v, j); }
 };
-__device__ __forceinline__ bool bit(uint64_t mask, int j) { return (mask >> j) & 1; }
+__device__ __forceinline__ uint32_t mask_of(bool b) { return (uint32_t)__ballot(b); }      // (of the first 32 lanes: one has WALK entries)
+__device__ __forceinline__ bool bit(uint32_t mask, int j) { return mask & 1u << j; }
 
 // values[chunk] (rows of `width`) is replaced by what step(entries, decay, value, result) puts into result, WALK chunks after WALK
 // chunks, down (UP: up) the program; decay = 2^(a2 steps[chunk]).
@@ -207,26 +210,19 @@ __device__ __forceinline__ void walk(const ScanArgs& a, float* values, const flo
   const uint32_t at = (uint32_t)w.at * 4u, c = (uint32_t)w.c * 4u;
   float value[WALK], len[WALK], result[WALK];
   Entries next;
-  auto request = [&](int u0) {                  // rows past the end are the last one again
+  auto request = [&](int u0) {
     Feed<float> x(values, w.width, u0), y(steps, a.channels, u0);
 #pragma unroll
     for (int j = 0; j < WALK; j++) {
-      const bool more = u0 + j < n - 1;
-      value[j] = x.next(at, more);
-      len[j] = y.next(c, more);
+      value[j] = x.next(at, true);
+      len[j] = y.next(c, true);
     }
     next.load(a, u0, with_cap);
   };
   auto store = [&](int u0) {
     Feed<float> x(values, w.width, u0);
-    if (u0 + WALK <= n) {
 #pragma unroll
-      for (int j = 0; j < WALK; j++, x.so += x.step) x.put(at, result[j]);
-    } else {
-#pragma unroll
-      for (int j = 0; j < WALK; j++, x.so += x.step)
-        if (u0 + j < n) x.put(at, result[j]);
-    }
+    for (int j = 0; j < WALK; j++, x.so += x.step) x.put(at, result[j]);
   };
   auto start_of = [&](int i) { return WALK * (UP ? blocks - 1 - i : i); };
   request(start_of(0));
@@ -257,8 +253,8 @@ __device__ __forceinline__ void walk_down(const ScanArgs& a, float* local, const
                                                     float (&entering)[WALK]) {
     // A saved state is read before the two entries in front have saved theirs: one that they save is taken from the registers.
     const int lane = threadIdx.x;
-    const uint64_t from_one = __ballot(e.src == -2 || (e.src >= 0 && lane >= 1 && e.src == e.dst1));
-    const uint64_t from_two = __ballot(e.src >= 0 && lane >= 2 && e.src == e.dst2), captured = __ballot(e.cap >= 0);
+    const uint32_t from_one = mask_of(e.src == -2 || (e.src >= 0 && lane >= 1 && e.src == e.dst1));
+    const uint32_t from_two = mask_of(e.src >= 0 && lane >= 2 && e.src == e.dst2), captured = mask_of(e.cap >= 0);
     const int from = e.src < 0 ? slots.first : e.src, to = e.dst < 0 ? slots.unread : e.dst;
     float saved[WALK], before = 0.f;
     saved[0] = slots[Entries::at(from, 0)];

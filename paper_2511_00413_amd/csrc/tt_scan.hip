@@ -124,15 +124,15 @@ size_t up(size_t v) { return (v + 255) & ~(size_t)255; }
 
 size_t scan_fwd_workspace(int channels, int n_state, int n_chunks, int n_slots) {
   const size_t width = (size_t)channels * n_state * sizeof(float);
-  return up(width * n_chunks) + up((size_t)channels * n_chunks * sizeof(float)) + up(width * (n_slots + EXTRA_SLOTS)) + 256;
+  return up(width * walk_rows(n_chunks)) + up(channels * walk_rows(n_chunks) * sizeof(float)) + up(width * (n_slots + EXTRA_SLOTS)) + 256;
 }
 
 hipError_t scan_fwd(const ScanArgs& a, hipStream_t st) {
   if (a.n_chunks == 0) return hipSuccess;
   const size_t width = (size_t)a.channels * a.n_state * sizeof(float);
   float* local = (float*)a.workspace;
-  float* steps = (float*)((char*)local + up(width * a.n_chunks));
-  float* slots = (float*)((char*)steps + up((size_t)a.channels * a.n_chunks * sizeof(float)));
+  float* steps = (float*)((char*)local + up(width * walk_rows(a.n_chunks)));
+  float* slots = (float*)((char*)steps + up(a.channels * walk_rows(a.n_chunks) * sizeof(float)));
   const int blocks = (a.channels + THREADS - 1) / THREADS;
   const unsigned grid = (unsigned)blocks * (unsigned)a.n_chunks;
   return by_type(a.bf16, a.n_state, [&](auto zero, auto ns) -> hipError_t {

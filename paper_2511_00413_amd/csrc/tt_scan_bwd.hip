@@ -121,9 +121,9 @@ scan_bwd_states_kernel(ScanArgs a, float* local, float* back, const float* __res
   float sent = 0.f;                                                            // by the chunk behind
   walk<true>(a, back, steps, w, a2, a.d_state_out != nullptr, [&](const Entries& e, const float (&decay)[WALK], const float (&own)[WALK],
                                                                   float (&leaving)[WALK]) {
-    const uint64_t continued = __ballot(e.src_behind == -2), saves = __ballot(e.dst >= 0), captured = __ballot(e.cap >= 0);
-    const uint64_t used = continued | saves | captured;                        // (steps are not there where no state is used)
-    const uint64_t starts = __ballot(e.src != -2);
+    const uint32_t continued = mask_of(e.src_behind == -2), saves = mask_of(e.dst >= 0), captured = mask_of(e.cap >= 0);
+    const uint32_t used = continued | saves | captured;                        // (steps are not there where no state is used)
+    const uint32_t starts = mask_of(e.src != -2);
     const int to = e.src < 0 ? slots.first : e.src;
     float given[WALK];
 #pragma unroll
@@ -423,7 +423,7 @@ int strips_of(int channels, int n_chunks) {
 size_t scan_bwd_workspace(int64_t n_tokens, int channels, int n_state, int n_chunks, int n_slots) {
   const size_t width = (size_t)channels * n_state * sizeof(float);
   const size_t blocks = (channels + WAVE - 1) / WAVE, strips = strips_of(channels, n_chunks);
-  return 2 * up(width * n_chunks) + up((size_t)channels * n_chunks * sizeof(float)) + up(2 * width * (n_slots + EXTRA_SLOTS)) +
+  return 2 * up(width * walk_rows(n_chunks)) + up(channels * walk_rows(n_chunks) * sizeof(float)) + up(2 * width * (n_slots + EXTRA_SLOTS)) +
          up(width * fronts(n_tokens)) + up((size_t)channels * fronts(n_tokens) * sizeof(float)) +
          up(blocks * n_tokens * 2 * n_state * sizeof(float)) + up(strips * width) + up(strips * 2 * channels * sizeof(float)) + 256;
 }
@@ -433,9 +433,9 @@ hipError_t scan_bwd(const ScanArgs& a, hipStream_t st) {
   const int blocks = (a.channels + WAVE - 1) / WAVE, strips = strips_of(a.channels, a.n_chunks);
   char* w = (char*)a.workspace;
   auto take = [&](size_t bytes) { float* p = (float*)w; w += up(bytes); return p; };
-  float* local = take(width * a.n_chunks);
-  float* back = take(width * a.n_chunks);
-  float* steps = take((size_t)a.channels * a.n_chunks * sizeof(float));
+  float* local = take(width * walk_rows(a.n_chunks));
+  float* back = take(width * walk_rows(a.n_chunks));
+  float* steps = take(a.channels * walk_rows(a.n_chunks) * sizeof(float));
   float* slots = take(2 * width * (a.n_slots + EXTRA_SLOTS));
   float* front_states = take(width * fronts(a.n_tokens));
   float* front_steps = take((size_t)a.channels * fronts(a.n_tokens) * sizeof(float));
