@@ -15,7 +15,7 @@
 // No atomics: every sum has a fixed order.  One lane holds one channel; the sums over a wave's 64 channels for the 2 NS entries of
 // dB and dC are taken together, the lanes halving the entries they keep at every step (70 instructions for 32 sums).
 //
-// Bound by the vector ALU, as the forward: 16406 tokens of 4096 channels, ends 279 us (105 % busy), states 65, grads 954 (87 %), sums 31.
+// Bound by the vector ALU, as the forward: 16406 tokens of 4096 channels, ends 285 us (106 % busy), states 61, grads 961 (87 %), sums 31.
 #include <algorithm>
 #include "tt_scan.h"
 
