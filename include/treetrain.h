@@ -423,7 +423,8 @@ tt_status tt_tree_rope(int64_t n_tokens, int32_t n_heads, int32_t d, int32_t dty
  *     Both NULL iff top_k == 0.
  *   logp, entropy [n_rows] fp32, required; lse [n_rows] fp32 or NULL (the gradient needs it).
  *   Entries at -inf have probability 0 and add nothing to the entropy; a row with a NaN, with an entry
- *   at +inf or with nothing above -inf gives NaN.  Sums are fp32 and their order is fixed.
+ *   at +inf or with nothing above -inf gives NaN.  Finite logits may have any size (masks, or rows far
+ *   from zero as a whole; those past 5.8e6 are read three times).  Sums are fp32 and their order is fixed.
  *   workspace: tt_tree_logprob_entropy_workspace bytes (few rows are worked on in parts), 16-byte
  *     aligned; 0 from that function means that the sizes are invalid.
  * Alignment: logits aligned to its element size.

@@ -1,6 +1,7 @@
 // Log-probability of given tokens with the entropy and the most probable alternatives, and the gradient of the first two.
 //
-// Per row of logits z, in powers of two (x = z log2 e) against a whole number r just above the maximum of x:
+// Per row of logits z, in powers of two (x = z log2 e) against a whole number r just above the maximum of x (by what its product
+// rounds, at most one below it):
 //   s = sum 2^(x - r),  u = sum 2^(x - r) (x - r);
 //   lse = ln 2 (r + log2 s),  logp = ln 2 ((x_y - r) - log2 s),  entropy = -sum p ln p = ln 2 (log2 s - u / s),
 // all in one pass over the row: when r becomes r', s becomes s f and u becomes f (u + s (r - r')), f = 2^(r - r').  r being whole, x - r
@@ -38,13 +39,15 @@ typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x8 __attribute__((ext_vector_type(8)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 
-__device__ __forceinline__ float ex2(float x) { return __builtin_amdgcn_exp2f(x); }     // arguments <= 0: what flushes to 0 is 0 in a sum
+__device__ __forceinline__ float ex2(float x) { return __builtin_amdgcn_exp2f(x); }     // arguments <= 1: what flushes to 0 is 0 in a sum
 
-// r starts below every row that this form is for: a row whose r ends up past +-EXTREME (logits of the type's lowest value
-// throughout, or near its largest, where x itself overflows) is done again by far_row.  A term far below r is 0 in s and, its exponent
-// cut at FAR, a zero in u as well.  NaN passes the maxima and stays in s.
+// r comes from the rounded product, x - r holds the exact one: what the rounding took, half a step of the largest x, is added to every
+// exponent.  Within +-2^24 that is at most one.  (Unbounded it is hundreds at masks of -1e10, whose exponentials overflow.)  So r starts
+// at START: logits below that, masks, add nothing and never set it; and a row whose r ends up past +-EXTREME, masked throughout or far
+// from zero as a whole, is done again by far_row.  A term far below r is 0 in s and, its exponent cut at FAR, a zero in u as well.
+// NaN passes the maxima and stays in s.
 struct Stat { float r, s, u; };
-constexpr float START = -1e30f, EXTREME = 1e29f, FAR = -300.f;
+constexpr float START = -0x1p24f, EXTREME = 0x1p23f, FAR = -300.f;
 
 __device__ __forceinline__ void raise(Stat& st, float r) {
   const float d = st.r - r, f = ex2(d);
@@ -165,7 +168,7 @@ struct Result {
   __device__ __forceinline__ float lse() const { return far ? ref + log_s : LN2 * (ref + log_s); }
   __device__ __forceinline__ float logp(float z) const {
     if (far) return (z - ref) - log_s;
-    if (!(fabsf(z) < EXTREME)) return z - lse();          // a masked logit, whose x overflows
+    if (!(fabsf(z) < EXTREME)) return z - lse();          // a masked logit: one rounding, where its x may overflow
     return LN2 * (fmaf(z, LOG2E, -ref) - log_s);
   }
 };
