@@ -434,7 +434,8 @@ tt_status tt_tree_rope(int64_t n_tokens, int32_t n_heads, int32_t d, int32_t dty
  *   one read of the logits, one write (dtype of the logits, rounded to nearest even).  lse and entropy
  *   are the forward's; d_logp, d_entropy [n_rows] fp32, each may be NULL (= 0).  Ignored rows get
  *   exactly zero (their logits, lse and upstream gradients are not read).  dlogits may be logits when
- *   the strides are equal; otherwise the two may not overlap.
+ *   the strides are equal; otherwise the two may not overlap.  p = exp(z - lse) is off by what lse is rounded by,
+ *   at most 2^-13 of it; rows with |lse| of 1024 and more are summed again (slower), and theirs is not.
  * Alignment: both arrays aligned to the element size; where logits and gradient rows are the same
  *   distance from a 16-byte boundary they go in vectors, otherwise element by element.
  * ------------------------------------------------------------------------------------------ */

@@ -144,16 +144,16 @@ struct Shared {
 };
 
 // The workgroup's sums from the threads': raised to the wave's maximum and added, then the same for the waves.
-__device__ Stat join(Shared& sh, Stat st) {
+__device__ Stat join(Stat (&part)[WAVES], Stat st) {
   raise(st, wave_all(st.r, [](float a, float b) { return fmaxf(a, b); }));
   st.s = wave_all(st.s, [](float a, float b) { return a + b; });
   st.u = wave_all(st.u, [](float a, float b) { return a + b; });
-  if ((threadIdx.x & 63) == 0) sh.part[threadIdx.x >> 6] = st;
+  if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = st;
   __syncthreads();
-  Stat all = {sh.part[0].r, 0.f, 0.f};
-  for (int w = 1; w < WAVES; w++) all.r = fmaxf(all.r, sh.part[w].r);
+  Stat all = {part[0].r, 0.f, 0.f};
+  for (int w = 1; w < WAVES; w++) all.r = fmaxf(all.r, part[w].r);
   for (int w = 0; w < WAVES; w++) {
-    Stat p = sh.part[w];
+    Stat p = part[w];
     raise(p, all.r);
     all.s += p.s;
     all.u += p.u;
@@ -173,17 +173,18 @@ struct Result {
   }
 };
 
-// The sums of a row of extreme logits against its maximum, differences taken before they are scaled: two more passes.
+// The sums of a row of extreme logits against its maximum, differences taken before they are scaled: two more passes.  A barrier lies
+// behind the last read of the row.
 template <typename T>
-__device__ Result far_row(Shared& sh, const T* row, int vocab) {
+__device__ Result far_row(Stat (&part)[WAVES], const T* row, int vocab) {
   const int t = threadIdx.x;
   float m = -INFINITY;
   for (int e = t; e < vocab; e += THREADS) m = fmaxf(m, Row<T>::at(row, e));
   m = wave_all(m, [](float a, float b) { return fmaxf(a, b); });
-  __syncthreads();                           // (the sums in sh.part have been read)
-  if ((t & 63) == 0) sh.part[t >> 6].r = m;
+  __syncthreads();                           // (the sums in part have been read)
+  if ((t & 63) == 0) part[t >> 6].r = m;
   __syncthreads();
-  for (int w = 0; w < WAVES; w++) m = fmaxf(m, sh.part[w].r);
+  for (int w = 0; w < WAVES; w++) m = fmaxf(m, part[w].r);
   Stat st = {0.f, 0.f, 0.f};
   for (int e = t; e < vocab; e += THREADS) {
     const float d = Row<T>::at(row, e) - m, p = ex2(d * LOG2E);
@@ -191,14 +192,14 @@ __device__ Result far_row(Shared& sh, const T* row, int vocab) {
     st.u = fmaf(p, fmaxf(d, FAR), st.u);
   }
   __syncthreads();
-  st = join(sh, st);
+  st = join(part, st);
   const float ln_s = LN2 * log2f(st.s);
   return {true, m, ln_s, ln_s - st.u / st.s};
 }
 
 template <typename T>
-__device__ __forceinline__ Result result_of(Shared& sh, const Stat& all, const T* row, int vocab) {
-  if (!(fabsf(all.r) < EXTREME)) return far_row(sh, row, vocab);          // (all threads hold the same r)
+__device__ __forceinline__ Result result_of(Stat (&part)[WAVES], const Stat& all, const T* row, int vocab) {
+  if (!(fabsf(all.r) < EXTREME)) return far_row(part, row, vocab);          // (all threads hold the same r)
   const float log_s = log2f(all.s);
   return {false, all.r, log_s, LN2 * (log_s - all.u / all.s)};
 }
@@ -347,10 +348,10 @@ entropy_rows_kernel(int64_t row0, int vocab, const T* __restrict__ logits, int64
   }
   if (last) for (int e = tail0 + t; e < vocab; e += THREADS) single(e);
 
-  const Stat all = join(sh, st);
+  const Stat all = join(sh.part, st);
   Result res{};
   if (parts == 1) {
-    res = result_of(sh, all, row, vocab);
+    res = result_of(sh.part, all, row, vocab);
     if (t == 0) {
       const int y = target[r];
       const bool used = y >= 0 && y < vocab;
@@ -443,9 +444,9 @@ entropy_join_kernel(int64_t row0, int vocab, const T* __restrict__ logits, int64
     st.s += q.s;
     st.u += q.u;
   }
-  const Stat all = join(sh, st);
+  const Stat all = join(sh.part, st);
   const T* row = logits + r * row_stride;
-  const Result res = result_of(sh, all, row, vocab);
+  const Result res = result_of(sh.part, all, row, vocab);
   if (t == 0) {
     const int y = target[r];
     const bool used = y >= 0 && y < vocab;
@@ -477,6 +478,10 @@ entropy_join_kernel(int64_t row0, int vocab, const T* __restrict__ logits, int64
 // ---- gradient ------------------------------------------------------------------------------------
 // A row is cut into parts of 16 KB, one workgroup each, four vectors in flight per thread.
 // Gradient and logits rows the same distance from a 16-byte boundary go in vectors behind a scalar head.
+// p = exp(z - lse) is off by what lse is rounded by, some |lse| 2^-23: 10^-4 of it at SUM_AGAIN (a twentieth of half a step in bf16), all
+// of it where ln s does not reach lse's last digit.  Rows from there on, which no trained model has, and rows without a distribution are
+// summed again by the workgroup of their first part, which then takes the whole row.
+constexpr float SUM_AGAIN = 1024.f;
 template <typename T>
 __global__ void __launch_bounds__(THREADS)
 entropy_bwd_kernel(int64_t row0, int vocab, const T* logits, int64_t row_stride, const int32_t* __restrict__ target,
@@ -493,6 +498,16 @@ entropy_bwd_kernel(int64_t row0, int vocab, const T* logits, int64_t row_stride,
   const float a = used && d_logp ? d_logp[r] : 0.f, b = used && d_entropy ? d_entropy[r] : 0.f;
   const float lse = used ? lse_in[r] : 0.f;
   const float c = a + b * (used ? entropy[r] : 0.f);
+  __shared__ Stat sums[WAVES];
+  if (used && !(fabsf(lse) < SUM_AGAIN)) {
+    if (part > 0) return;
+    const Result res = far_row(sums, row, vocab);
+    for (int e = t; e < vocab; e += THREADS) {
+      const float d = res.logp(Row<T>::at(row, e));
+      Row<T>::put(out, e, -ex2(d * LOG2E) * fmaf(b, fmaxf(d, FAR), c) + (e == y ? a : 0.f));
+    }
+    return;
+  }
   const bool vec_ok = ((reinterpret_cast<uintptr_t>(row) ^ reinterpret_cast<uintptr_t>(out)) & 15) == 0;
   const int head = vec_ok ? min((int)(((16 - (reinterpret_cast<uintptr_t>(row) & 15)) & 15) / sizeof(T)), vocab) : 0;
   const int nvec = vec_ok ? (vocab - head) / EPV : 0;
