@@ -1,4 +1,9 @@
-"""ctypes binding of libtreetrain.so.  Argument marshalling only."""
+"""ctypes binding of libtreetrain.so.  Argument marshalling only.
+
+Streams: a call queues its work on the current stream, or on the torch.cuda.Stream that it is given as `stream`.  The inputs have to be
+ready on that stream and to stay until it is through with them; outputs are used on another stream behind an event or a wait of it, as
+for any work on a stream of one's own.
+"""
 from __future__ import annotations
 
 import ctypes
@@ -384,8 +389,8 @@ class GdnPlan:
             self.scan_programs[(channels, backward)] = prog
         return prog
 
-    def _scan_chunks(self, channels: int, backward: bool, device, captured: bool, stream):
-        """ctypes tt_scan_chunks of that program on `device`, for a call on `stream` (None: the current one)."""
+    def _scan_chunks(self, channels: int, backward: bool, device, captured: bool):
+        """ctypes tt_scan_chunks of that program on `device`, for a call on the current stream."""
         prog = self._scan_program(channels, backward)
         key = (channels, backward, device)
         on_device = self.scan_programs.get(key)
@@ -397,8 +402,8 @@ class GdnPlan:
             rows, n = [packed[i].data_ptr() for i in range(6)], prog.shape[1]
             on_device = self.scan_programs[key] = (packed, _ScanChunks(n, self.n_slots, *rows[:4], None, rows[5]),
                                                    _ScanChunks(n, self.n_slots, *rows), _stream_ptr(None))
-        if _stream_ptr(stream) != on_device[3]:      # not reused, once the plan is dropped, before that stream is through with it
-            on_device[0].record_stream(_torch().cuda.current_stream() if stream is None else stream)
+        if _stream_ptr(None) != on_device[3]:        # not reused, once the plan is dropped, before this stream is through with it
+            on_device[0].record_stream(_torch().cuda.current_stream())
         return on_device[2 if captured else 1]
 
     def _schedule(self):
@@ -646,18 +651,31 @@ def _enter_device(*tensors):
     return before
 
 
-def _new(like, shape, stream, dtype=None):
-    """An empty tensor on the device of `like` (and of its dtype) for a call on `stream` (None: the current one): not reused, once
-    dropped, before that stream is through."""
+def _new(like, shape, dtype=None):
+    """An empty tensor on the device of `like` (and of its dtype)."""
     if dtype is not None:
-        t = like.new_empty(shape, dtype=dtype)
-    elif like.shape == shape and like.is_contiguous():
-        t = _TORCH.empty_like(like)                       # the quickest of the three
-    else:
-        t = like.new_empty(shape)
-    if stream is not None:
-        t.record_stream(stream)
-    return t
+        return like.new_empty(shape, dtype=dtype)
+    if like.shape == shape and like.is_contiguous():
+        return _TORCH.empty_like(like)                    # the quickest of the three
+    return like.new_empty(shape)
+
+
+def _on_stream(stream, call, arguments):
+    """call(**arguments) with the `stream` among them as the current one, so that what the call allocates is that stream's memory.  (Memory
+    of the stream that is current now may just have been dropped by work that is still queued there, and nothing orders the call behind
+    that work.)  What is returned is not handed out again, once dropped, before the stream that is current now is through with it."""
+    torch = _torch()
+    del arguments["stream"]
+    for t in arguments.values():
+        if isinstance(t, torch.Tensor) and t.get_device() != stream.device_index:
+            raise ValueError(f"a tensor on {t.device} in a call on a stream of cuda:{stream.device_index}")
+    here = torch.cuda.current_stream(stream.device_index)
+    with torch.cuda.stream(stream):
+        out = call(**arguments)
+    for t in out if isinstance(out, tuple) else (out,):
+        if t is not None:
+            t.record_stream(here)
+    return out
 
 
 def _leave_device(before):
@@ -768,6 +786,8 @@ def tree_rope_axes(x, axis_pos, sections, *, interleaved: bool = False, theta_ba
     stride), axis_pos [n_axes, n] int32, 1 to 4 axes.  sections: pairs of every axis, d/2 together; the first axis has the first
     pairs and so on or, interleaved, pair i belongs to axis i % n_axes while that axis has had fewer pairs than its section, and
     to the first axis otherwise.  `inverse` undoes the rotation / is its backward; `out` may be x (in place)."""
+    if stream is not None:
+        return _on_stream(stream, tree_rope_axes, locals())
     torch = _torch()
     if x.dim() != 3 or axis_pos.dim() != 2:
         raise ValueError("x must be [tokens, heads, d], axis_pos [axes, tokens]")
@@ -786,10 +806,10 @@ def tree_rope_axes(x, axis_pos, sections, *, interleaved: bool = False, theta_ba
     before = _enter_device(x, axis_pos, out)
     try:
         if out is None:
-            out = _new(x, (n, h, d), stream)
+            out = _new(x, (n, h, d))
         _check(_lib().tt_tree_rope_axes(n, h, d, DTYPE_BF16 if x.dtype == torch.bfloat16 else DTYPE_FP32, _dp(x), stride, n_axes,
                                         _dp(axis_pos), pair_axis, float(theta_base), 1 if inverse else 0, _dp(out), out_stride,
-                                        _stream_ptr(stream)))
+                                        _stream_ptr(None)))
     finally:
         _leave_device(before)
     return out
@@ -838,6 +858,8 @@ def tree_logprob_entropy(logits, target, *, top_k: int = 0, logp=None, entropy=N
     the row's distribution, its log-sum-exp, and the top_k (at most 64) most probable entries.  Returns (logp [n], entropy [n],
     lse [n] fp32, top_index [n, top_k] int32, top_logp [n, top_k] fp32), the last two None when top_k is 0: indices by falling
     log-prob, the lowest index first among equals.  A row whose target lies outside [0, V) is ignored: logp and entropy are 0."""
+    if stream is not None:
+        return _on_stream(stream, tree_logprob_entropy, locals())
     torch = _torch()
     code, (n, vocab) = _logits_dtype(logits), logits.shape
     stride = _check_rows(logits, "logits", (n, vocab), (torch.bfloat16, torch.float32))
@@ -855,17 +877,17 @@ def tree_logprob_entropy(logits, target, *, top_k: int = 0, logp=None, entropy=N
         _check_tensor(top_logp, "top_logp", (n, top_k), torch.float32)
     before = _enter_device(logits, target, logp, entropy, lse, top_index, top_logp, workspace)
     try:
-        logp = _new(logits, (n,), stream, torch.float32) if logp is None else logp
-        entropy = _new(logp, (n,), stream) if entropy is None else entropy
-        lse = _new(logp, (n,), stream) if lse is None else lse
+        logp = _new(logits, (n,), torch.float32) if logp is None else logp
+        entropy = _new(logp, (n,)) if entropy is None else entropy
+        lse = _new(logp, (n,)) if lse is None else lse
         if top_k:
-            top_logp = _new(logp, (n, top_k), stream) if top_logp is None else top_logp
-            top_index = _new(top_logp, (n, top_k), stream, torch.int32) if top_index is None else top_index
+            top_logp = _new(logp, (n, top_k)) if top_logp is None else top_logp
+            top_index = _new(top_logp, (n, top_k), torch.int32) if top_index is None else top_index
         if workspace is None:
-            workspace = _new(logits, (need,), stream, torch.uint8)
+            workspace = _new(logits, (need,), torch.uint8)
         _check(_lib().tt_tree_logprob_entropy(n, vocab, code, _dp(logits), stride, _dp(target), top_k, _dp(logp), _dp(entropy),
                                               _dp(lse), _dp(top_index), _dp(top_logp), _dp(workspace),
-                                              workspace.numel() * workspace.element_size(), _stream_ptr(stream)))
+                                              workspace.numel() * workspace.element_size(), _stream_ptr(None)))
     finally:
         _leave_device(before)
     return logp, entropy, lse, top_index, top_logp
@@ -875,6 +897,8 @@ def tree_logprob_entropy_bwd(logits, target, lse, entropy, d_logp=None, d_entrop
     """Gradient of sum(d_logp * logp + d_entropy * entropy) with respect to the logits, in their dtype and shape; lse and entropy
     [n] are the ones tree_logprob_entropy returned, d_logp and d_entropy [n] fp32 (None = 0).  Rows whose target lies outside
     [0, V) get zero.  `out` may be the logits tensor itself (in place)."""
+    if stream is not None:
+        return _on_stream(stream, tree_logprob_entropy_bwd, locals())
     torch = _torch()
     code, (n, vocab) = _logits_dtype(logits), logits.shape
     stride = _check_rows(logits, "logits", (n, vocab), (torch.bfloat16, torch.float32))
@@ -890,9 +914,9 @@ def tree_logprob_entropy_bwd(logits, target, lse, entropy, d_logp=None, d_entrop
     before = _enter_device(logits, target, lse, entropy, d_logp, d_entropy, out)
     try:
         if out is None:
-            out = _new(logits, (n, vocab), stream)
+            out = _new(logits, (n, vocab))
         _check(_lib().tt_tree_logprob_entropy_bwd(n, vocab, code, _dp(logits), stride, _dp(target), _dp(lse), _dp(entropy),
-                                                  _dp(d_logp), _dp(d_entropy), _dp(out), out_stride, _stream_ptr(stream)))
+                                                  _dp(d_logp), _dp(d_entropy), _dp(out), out_stride, _stream_ptr(None)))
     finally:
         _leave_device(before)
     return out
@@ -1210,6 +1234,8 @@ def tree_scan_fwd(x, dt, A, B, C, plan: GdnPlan, *, D=None, z=None, dt_bias=None
     chunk program is tree_gdn_plan's, whose first call with these many channels copies it to the device (so not one that a graph
     captures).  Returns y [n, channels]; with return_states also the end states [n_capture, channels, states] fp32 of the plan's
     capture nodes.  initial_state [channels, states] fp32: the state every root starts from."""
+    if stream is not None:
+        return _on_stream(stream, tree_scan_fwd, locals())
     torch = _torch()
     desc = _scan_desc(x, dt, A, B, C, D, z, dt_bias, softplus)
     n, ch, m = desc.n_tokens, desc.channels, desc.n_state
@@ -1221,16 +1247,16 @@ def tree_scan_fwd(x, dt, A, B, C, plan: GdnPlan, *, D=None, z=None, dt_bias=None
     try:
         dev = x.device
         captured = return_states and plan.n_capture > 0
-        chunks = plan._scan_chunks(ch, False, dev, captured, stream)
+        chunks = plan._scan_chunks(ch, False, dev, captured)
         if out is None:
-            out = _new(x, (n, ch), stream)
-        states = _new(A, (plan.n_capture, ch, m), stream) if return_states else None
+            out = _new(x, (n, ch))
+        states = _new(A, (plan.n_capture, ch, m)) if return_states else None
         need = int(_lib().tt_tree_scan_fwd_workspace(ctypes.byref(desc), chunks.n_chunks, chunks.n_slots))
         if workspace is None:
-            workspace = _new(x, (max(need, 256),), stream, torch.uint8)
+            workspace = _new(x, (max(need, 256),), torch.uint8)
         _check(_lib().tt_tree_scan_fwd(ctypes.byref(desc), ctypes.byref(chunks), _dp(x), _dp(dt), _dp(A), _dp(B), _dp(C), _dp(D), _dp(z),
                                        _dp(dt_bias), _dp(initial_state), _dp(states) if captured else None, _dp(out), _dp(workspace),
-                                       workspace.numel() * workspace.element_size(), _stream_ptr(stream)))
+                                       workspace.numel() * workspace.element_size(), _stream_ptr(None)))
     finally:
         _leave_device(before)
     return (out, states) if return_states else out
@@ -1249,6 +1275,8 @@ def tree_scan_bwd(x, dt, A, B, C, d_y, plan: GdnPlan, *, D=None, z=None, dt_bias
     """Backward of tree_scan_fwd for upstream d_y [n, channels] (dtype of x, free token stride).  d_state_out [n_capture, channels,
     states] fp32: upstream gradient of the plan's captured end states.  Returns ScanGrads: dx, ddt, dz like x, dB, dC like B, dA,
     dD, ddt_bias, d_initial_state fp32."""
+    if stream is not None:
+        return _on_stream(stream, tree_scan_bwd, locals())
     torch = _torch()
     desc = _scan_desc(x, dt, A, B, C, D, z, dt_bias, softplus)
     n, ch, m, groups = desc.n_tokens, desc.channels, desc.n_state, desc.groups
@@ -1262,16 +1290,16 @@ def tree_scan_bwd(x, dt, A, B, C, d_y, plan: GdnPlan, *, D=None, z=None, dt_bias
     try:
         dev = x.device
         captured = d_state_out is not None and plan.n_capture > 0
-        chunks = plan._scan_chunks(ch, True, dev, captured, stream)
-        like = lambda t: None if t is None else _new(t, t.shape, stream)      # noqa: E731
+        chunks = plan._scan_chunks(ch, True, dev, captured)
+        like = lambda t: None if t is None else _new(t, t.shape)      # noqa: E731
         grads = ScanGrads(like(x), like(x), like(A), like(B), like(C), like(D), like(z), like(dt_bias), like(A) if want_d_initial_state else None)
         need = int(_lib().tt_tree_scan_bwd_workspace(ctypes.byref(desc), chunks.n_chunks, chunks.n_slots))
         if workspace is None:
-            workspace = _new(x, (max(need, 256),), stream, torch.uint8)
+            workspace = _new(x, (max(need, 256),), torch.uint8)
         _check(_lib().tt_tree_scan_bwd(ctypes.byref(desc), ctypes.byref(chunks), _dp(x), _dp(dt), _dp(A), _dp(B), _dp(C), _dp(D), _dp(z),
                                        _dp(dt_bias), _dp(initial_state), _dp(d_y), _dp(d_state_out) if captured else None,
                                        *(_dp(g) for g in grads), _dp(workspace), workspace.numel() * workspace.element_size(),
-                                       _stream_ptr(stream)))
+                                       _stream_ptr(None)))
     finally:
         _leave_device(before)
     return grads
@@ -1283,6 +1311,8 @@ def tree_scan_step(x, dt, A, B, C, state, *, index=None, D=None, z=None, dt_bias
     [slots, channels, states] fp32.  Row r goes on from state index[r] (int32; several rows may share one, an index outside the
     states starts from zero) or, without an index, from state r.  Returns (y [rows, channels], state_out [rows, channels, states]);
     state_out may be state itself (in place) when there is no index."""
+    if stream is not None:
+        return _on_stream(stream, tree_scan_step, locals())
     torch = _torch()
     desc = _scan_desc(x, dt, A, B, C, D, z, dt_bias, softplus)
     n, ch, m = desc.n_tokens, desc.channels, desc.n_state
@@ -1296,11 +1326,11 @@ def tree_scan_step(x, dt, A, B, C, state, *, index=None, D=None, z=None, dt_bias
     before = _enter_device(x, dt, A, B, C, D, z, dt_bias, state, index, state_out, out)
     try:
         if out is None:
-            out = _new(x, (n, ch), stream)
+            out = _new(x, (n, ch))
         if state_out is None:
-            state_out = _new(state, (n, ch, m), stream)
+            state_out = _new(state, (n, ch, m))
         _check(_lib().tt_tree_scan_step(ctypes.byref(desc), _dp(x), _dp(dt), _dp(A), _dp(B), _dp(C), _dp(D), _dp(z), _dp(dt_bias), slots,
-                                        _dp(state), _dp(index), _dp(state_out), _dp(out), _stream_ptr(stream)))
+                                        _dp(state), _dp(index), _dp(state_out), _dp(out), _stream_ptr(None)))
     finally:
         _leave_device(before)
     return out, state_out
@@ -1310,6 +1340,8 @@ def tree_conv_step(x, state, weight, bias=None, *, index=None, silu: bool = True
     """One token per row: tree_conv_fwd from saved contexts.  x [rows, C] bf16/fp32 (free row stride), state [slots, K-1, C] like x:
     the inputs before the token, the oldest first; weight [C, K], bias [C] fp32.  index and state_out as in tree_scan_step.
     Returns (y [rows, C], state_out [rows, K-1, C])."""
+    if stream is not None:
+        return _on_stream(stream, tree_conv_step, locals())
     torch = _torch()
     if x.dim() != 2 or weight.dim() != 2:
         raise ValueError("x must be [rows, channels], weight [channels, taps]")
@@ -1329,12 +1361,12 @@ def tree_conv_step(x, state, weight, bias=None, *, index=None, silu: bool = True
     before = _enter_device(x, state, weight, bias, index, state_out, out)
     try:
         if out is None:
-            out = _new(x, (n, c), stream)
+            out = _new(x, (n, c))
         if state_out is None:
-            state_out = _new(state, (n, k - 1, c), stream)
+            state_out = _new(state, (n, k - 1, c))
         _check(_lib().tt_tree_conv_step(n, c, k, DTYPE_BF16 if x.dtype == torch.bfloat16 else DTYPE_FP32, 1 if silu else 0, _dp(x), xs,
                                         _dp(weight), _dp(bias), slots, _dp(state), _dp(index), _dp(state_out), _dp(out), ys,
-                                        _stream_ptr(stream)))
+                                        _stream_ptr(None)))
     finally:
         _leave_device(before)
     return out, state_out

@@ -184,3 +184,19 @@ def test_every_kernel_has_a_name():
     text = open(os.path.join(ROOT, "include", "treetrain.h")).read()
     assert int(re.search(r"#define TT_N_KERNELS\s+(\d+)", text).group(1)) == len(B.KERNEL_NAMES)
     assert int(re.search(r"#define TT_LOGPROB_TOP_MAX (\d+)", text).group(1)) == T.LOGPROB_TOP_MAX
+
+
+def test_a_stream_of_another_device():
+    """Tensors (here: on the CPU) that are not on the device of the stream that the call is given."""
+    from types import SimpleNamespace
+    other = SimpleNamespace(device_index=1, cuda_stream=64)
+    z, y, f32 = torch.zeros(4, 50), torch.zeros(4, dtype=torch.int32), lambda *s: torch.zeros(s)
+    plan = T.tree_gdn_plan([-1], [6])
+    x, A, Bc = f32(6, 64), f32(64, 16), f32(6, 1, 16)
+    for call in (lambda: T.tree_logprob_entropy(z, y, stream=other), lambda: T.tree_logprob_entropy_bwd(z, y, f32(4), f32(4), stream=other),
+                 lambda: T.tree_rope_axes(f32(6, 2, 32), torch.zeros(3, 6, dtype=torch.int32), (4, 6, 6), stream=other),
+                 lambda: T.tree_scan_fwd(x, x, A, Bc, Bc, plan, stream=other), lambda: T.tree_scan_bwd(x, x, A, Bc, Bc, x, plan, stream=other),
+                 lambda: T.tree_scan_step(x, x, A, Bc, Bc, f32(6, 64, 16), stream=other),
+                 lambda: T.tree_conv_step(x, f32(6, 3, 64), f32(64, 4), stream=other)):
+        with pytest.raises(ValueError, match="stream of cuda:1"):
+            call()
