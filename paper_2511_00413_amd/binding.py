@@ -687,6 +687,8 @@ def tree_attn_fwd(q, k, v, kend, kt_min, kt_max, *, k_prefix=None, v_prefix=None
                   o=None, lse=None, workspace=None, stream=None, reference_kernels: bool = False):
     """q [N,hq,d]; k, v [N,hkv,d]; kend/kt_min/kt_max: int32 device tensors from tree_build_meta.
     Returns (o [N,hq,d], lse [hq,N] fp32)."""
+    if stream is not None:
+        return _on_stream(stream, tree_attn_fwd, locals())
     torch = _torch()
     n_prefix = 0 if k_prefix is None else k_prefix.shape[0]
     desc = _desc(q, k, v, n_prefix, scale, reference_kernels)
@@ -699,7 +701,7 @@ def tree_attn_fwd(q, k, v, kend, kt_min, kt_max, *, k_prefix=None, v_prefix=None
     workspace, ws_bytes = _workspace(desc, False, workspace, q.device)
     _check(_lib().tt_tree_attn_fwd(ctypes.byref(desc), _dp(q), _dp(k), _dp(v), _dp(k_prefix), _dp(v_prefix),
                                    _dp(kend), _dp(kt_min), _dp(kt_max), _dp(o), _dp(lse),
-                                   _dp(workspace), ws_bytes, _stream_ptr(stream)))
+                                   _dp(workspace), ws_bytes, _stream_ptr(None)))
     return o, lse
 
 
@@ -708,6 +710,8 @@ def tree_attn_bwd(q, k, v, kend, kt_min, kt_max, o, d_o, lse, *, k_prefix=None, 
                   workspace=None, stream=None, reference_kernels: bool = False):
     """Returns (dq [N,hq,d], dk [N,hkv,d], dv [N,hkv,d]); prefix gradients are added into the fp32
     accumulators dk_prefix_acc / dv_prefix_acc [P,hkv,d]."""
+    if stream is not None:
+        return _on_stream(stream, tree_attn_bwd, locals())
     torch = _torch()
     n_prefix = 0 if k_prefix is None else k_prefix.shape[0]
     desc = _desc(q, k, v, n_prefix, scale, reference_kernels)
@@ -725,7 +729,7 @@ def tree_attn_bwd(q, k, v, kend, kt_min, kt_max, o, d_o, lse, *, k_prefix=None, 
     _check(_lib().tt_tree_attn_bwd(ctypes.byref(desc), _dp(q), _dp(k), _dp(v), _dp(k_prefix), _dp(v_prefix),
                                    _dp(kend), _dp(kt_min), _dp(kt_max), _dp(o), _dp(d_o), _dp(lse),
                                    _dp(dq), _dp(dk), _dp(dv), _dp(dk_prefix_acc), _dp(dv_prefix_acc),
-                                   _dp(workspace), ws_bytes, _stream_ptr(stream)))
+                                   _dp(workspace), ws_bytes, _stream_ptr(None)))
     return dq, dk, dv
 
 
@@ -733,6 +737,8 @@ def tree_weighted_logprob(logits, target, weight=None, *, loss_acc=None, logp=No
                           want_lse: bool = True, stream=None):
     """logits [n, V] bf16/fp32 (row stride free), target [n] int32, weight [n] fp32 or None.
     Returns (logp [n], lse [n] or None, loss_acc [1]); loss_acc is added to (zeroed if created here)."""
+    if stream is not None:
+        return _on_stream(stream, tree_weighted_logprob, locals())
     torch = _torch()
     if logits.dim() != 2 or logits.stride(1) != 1:
         raise ValueError("logits must be [rows, vocab] with contiguous vocab")
@@ -748,13 +754,15 @@ def tree_weighted_logprob(logits, target, weight=None, *, loss_acc=None, logp=No
     _check(_lib().tt_tree_weighted_logprob(
         n, vocab, DTYPE_BF16 if logits.dtype == torch.bfloat16 else DTYPE_FP32, _dp(logits),
         logits.stride(0) if n > 1 else vocab, _dp(target), _dp(weight), _dp(logp), _dp(lse), _dp(loss_acc),
-        _stream_ptr(stream)))
+        _stream_ptr(None)))
     return logp, lse, loss_acc
 
 
 def tree_rope(x, tok_pos, *, theta_base: float = 1.0e6, inverse: bool = False, out=None, stream=None):
     """Rotary embedding of x [n, heads, d] (bf16/fp32, heads and d contiguous, free token stride) with the
     tree position ids tok_pos [n] int32; `inverse` undoes it / is its backward.  `out` may be x (in place)."""
+    if stream is not None:
+        return _on_stream(stream, tree_rope, locals())
     torch = _torch()
     if x.dim() != 3 or x.stride(2) != 1 or (x.shape[1] > 1 and x.stride(1) != x.shape[2]):
         raise ValueError("x must be [tokens, heads, d] with heads and d contiguous")
@@ -767,7 +775,7 @@ def tree_rope(x, tok_pos, *, theta_base: float = 1.0e6, inverse: bool = False, o
         raise ValueError("out must match x in shape and dtype, heads and d contiguous")
     _check(_lib().tt_tree_rope(n, h, d, DTYPE_BF16 if x.dtype == torch.bfloat16 else DTYPE_FP32, _dp(x),
                                x.stride(0) if n > 1 else h * d, _dp(tok_pos), float(theta_base), 1 if inverse else 0,
-                               _dp(out), out.stride(0) if n > 1 else h * d, _stream_ptr(stream)))
+                               _dp(out), out.stride(0) if n > 1 else h * d, _stream_ptr(None)))
     return out
 
 
@@ -926,6 +934,8 @@ def tree_weighted_logprob_bwd(logits, target, weight, lse, *, grad_scale: float 
     """dlogits = grad_scale * weight * (softmax(logits) - onehot(target)), same dtype and shape as logits
     (zero rows where target < 0); lse [n] fp32 is the one tree_weighted_logprob returned.  `out` may be
     the logits tensor itself (in place)."""
+    if stream is not None:
+        return _on_stream(stream, tree_weighted_logprob_bwd, locals())
     torch = _torch()
     if logits.dim() != 2 or logits.stride(1) != 1:
         raise ValueError("logits must be [rows, vocab] with contiguous vocab")
@@ -939,7 +949,7 @@ def tree_weighted_logprob_bwd(logits, target, weight, lse, *, grad_scale: float 
     _check(_lib().tt_tree_weighted_logprob_bwd(
         n, vocab, DTYPE_BF16 if logits.dtype == torch.bfloat16 else DTYPE_FP32, _dp(logits),
         logits.stride(0) if n > 1 else vocab, _dp(target), _dp(weight), _dp(lse), float(grad_scale), _dp(out),
-        out.stride(0) if n > 1 else vocab, _stream_ptr(stream)))
+        out.stride(0) if n > 1 else vocab, _stream_ptr(None)))
     return out
 
 
@@ -947,6 +957,8 @@ def tree_weighted_logprob_fwd_bwd(logits, target, weight=None, *, grad_scale: fl
                                   lse=None, out=None, stream=None):
     """tree_weighted_logprob and tree_weighted_logprob_bwd in one pass over the logits.  Returns (logp [n], lse [n],
     loss_acc [1] (added to; zeroed if created here), dlogits like logits); `out` may be the logits tensor itself."""
+    if stream is not None:
+        return _on_stream(stream, tree_weighted_logprob_fwd_bwd, locals())
     torch = _torch()
     if logits.dim() != 2 or logits.stride(1) != 1:
         raise ValueError("logits must be [rows, vocab] with contiguous vocab")
@@ -967,7 +979,7 @@ def tree_weighted_logprob_fwd_bwd(logits, target, weight=None, *, grad_scale: fl
     _check(_lib().tt_tree_weighted_logprob_fwd_bwd(
         n, vocab, DTYPE_BF16 if logits.dtype == torch.bfloat16 else DTYPE_FP32, _dp(logits),
         logits.stride(0) if n > 1 else vocab, _dp(target), _dp(weight), float(grad_scale), _dp(logp), _dp(lse), _dp(loss_acc),
-        _dp(out), out.stride(0) if n > 1 else vocab, _stream_ptr(stream)))
+        _dp(out), out.stride(0) if n > 1 else vocab, _stream_ptr(None)))
     return logp, lse, loss_acc, out
 
 
@@ -992,6 +1004,8 @@ def tree_attn_partitioned_fwd(q, k, v, plan: PartitionPlan, *, scale=None, o=Non
                               stream=None, reference_kernels: bool = False):
     """Whole-tree q [N,hq,d], k, v [N,hkv,d] in whole-tree DFS order; one attention pass per partition of
     `plan`.  Returns (o [N,hq,d], lse [hq,N])."""
+    if stream is not None:
+        return _on_stream(stream, tree_attn_partitioned_fwd, locals())
     torch = _torch()
     desc = _desc(q, k, v, 0, scale, reference_kernels)
     cplan = plan._c()
@@ -1001,13 +1015,15 @@ def tree_attn_partitioned_fwd(q, k, v, plan: PartitionPlan, *, scale=None, o=Non
         lse = torch.empty((desc.hq, desc.n_q), dtype=torch.float32, device=q.device)
     workspace, ws_bytes = _part_workspace(desc, cplan, False, workspace, q.device)
     _check(_lib().tt_tree_attn_partitioned_fwd(ctypes.byref(desc), ctypes.byref(cplan), _dp(q), _dp(k), _dp(v),
-                                               _dp(o), _dp(lse), _dp(workspace), ws_bytes, _stream_ptr(stream)))
+                                               _dp(o), _dp(lse), _dp(workspace), ws_bytes, _stream_ptr(None)))
     return o, lse
 
 
 def tree_attn_partitioned_bwd(q, k, v, plan: PartitionPlan, o, d_o, lse, *, scale=None, dq=None, dk=None, dv=None,
                               workspace=None, stream=None, reference_kernels: bool = False):
     """Returns whole-tree (dq, dk, dv); cached-key gradients of all partitions are summed in fp32 inside."""
+    if stream is not None:
+        return _on_stream(stream, tree_attn_partitioned_bwd, locals())
     torch = _torch()
     desc = _desc(q, k, v, 0, scale, reference_kernels)
     cplan = plan._c()
@@ -1022,7 +1038,7 @@ def tree_attn_partitioned_bwd(q, k, v, plan: PartitionPlan, o, d_o, lse, *, scal
     workspace, ws_bytes = _part_workspace(desc, cplan, True, workspace, q.device)
     _check(_lib().tt_tree_attn_partitioned_bwd(ctypes.byref(desc), ctypes.byref(cplan), _dp(q), _dp(k), _dp(v),
                                                _dp(o), _dp(d_o), _dp(lse), _dp(dq), _dp(dk), _dp(dv),
-                                               _dp(workspace), ws_bytes, _stream_ptr(stream)))
+                                               _dp(workspace), ws_bytes, _stream_ptr(None)))
     return dq, dk, dv
 
 
@@ -1044,18 +1060,22 @@ def _row_stride(t):
 def tree_conv_fwd(x, weight, bias, tok_pred, *, silu: bool = True, out=None, stream=None):
     """Tree-correct depthwise causal conv: x [n, C] bf16/fp32, weight [C, K] fp32, bias [C] fp32 or None,
     tok_pred [n] int32 (from tree_build_meta).  Returns y [n, C]."""
+    if stream is not None:
+        return _on_stream(stream, tree_conv_fwd, locals())
     torch = _torch()
     n, c, k, dt = _conv_check(x, weight)
     if out is None:
         out = torch.empty((n, c), dtype=x.dtype, device=x.device)
     _check(_lib().tt_tree_conv_fwd(n, c, k, dt, 1 if silu else 0, _dp(x), _row_stride(x), _dp(weight), _dp(bias), _dp(tok_pred),
-                                   _dp(out), _row_stride(out), _stream_ptr(stream)))
+                                   _dp(out), _row_stride(out), _stream_ptr(None)))
     return out
 
 
 def tree_conv_bwd(x, weight, bias, tok_pred, dy, plan: ConvPlan, *, silu: bool = True, want_dbias: bool = True,
                   workspace=None, stream=None):
     """Returns (dx [n, C] in x's dtype, dweight [C, K] fp32, dbias [C] fp32 or None)."""
+    if stream is not None:
+        return _on_stream(stream, tree_conv_bwd, locals())
     torch = _torch()
     n, c, k, dt = _conv_check(x, weight)
     _conv_check(dy, weight, "dy")
@@ -1073,7 +1093,7 @@ def tree_conv_bwd(x, weight, bias, tok_pred, dy, plan: ConvPlan, *, silu: bool =
     _check(_lib().tt_tree_conv_bwd(n, c, k, dt, 1 if silu else 0, _dp(x), _row_stride(x), _dp(weight), _dp(bias), _dp(tok_pred),
                                    _dp(dy), _row_stride(dy), len(plan.fix_tok), _dp(d["fix_tok"]), _dp(d["fix_off"]),
                                    _dp(d["fix_t"]), _dp(d["fix_r"]), _dp(dx), _row_stride(dx), _dp(dw), _dp(db),
-                                   _dp(workspace), workspace.numel(), _stream_ptr(stream)))
+                                   _dp(workspace), workspace.numel(), _stream_ptr(None)))
     return dx, dw, db
 
 
@@ -1085,6 +1105,8 @@ def tree_conv_bwd_static(x, weight, bias, tok_pred, dy, plan: ConvPlan, dx, dwei
     """tree_conv_bwd for callers that may not allocate: every output is passed in (dx [n, C] in x's dtype,
     dweight [C, K] fp32, dbias [C] fp32 or None), the plan must already be on the device, and the scratch is the
     library's static array (shapes whose scratch exceeds CONV_BWD_STATIC_SCRATCH_BYTES are refused)."""
+    if stream is not None:
+        return _on_stream(stream, tree_conv_bwd_static, locals())
     n, c, k, dt = _conv_check(x, weight)
     _conv_check(dy, weight, "dy")
     if plan.kernel_size != k:
@@ -1097,7 +1119,7 @@ def tree_conv_bwd_static(x, weight, bias, tok_pred, dy, plan: ConvPlan, dx, dwei
     _check(_lib().tt_tree_conv_bwd_static(n, c, k, dt, 1 if silu else 0, _dp(x), _row_stride(x), _dp(weight), _dp(bias),
                                           _dp(tok_pred), _dp(dy), _row_stride(dy), len(plan.fix_tok), _dp(d["fix_tok"]),
                                           _dp(d["fix_off"]), _dp(d["fix_t"]), _dp(d["fix_r"]), _dp(dx), _row_stride(dx),
-                                          _dp(dweight), _dp(dbias), _stream_ptr(stream)))
+                                          _dp(dweight), _dp(dbias), _stream_ptr(None)))
 
 
 def tree_gdn_fwd(q, k, v, g, beta, plan: GdnPlan, *, scale=None, out=None, workspace=None, stream=None,
@@ -1106,6 +1128,8 @@ def tree_gdn_fwd(q, k, v, g, beta, plan: GdnPlan, *, scale=None, out=None, works
     [n, hv] fp32 (g = log decay <= 0).  Returns o [n, hv, 128] bf16; with return_states also the end states
     [n_capture, hv, 128, 128] fp32 of the plan's capture nodes.  initial_state [hv, 128, 128] fp32: the state
     every root starts from."""
+    if stream is not None:
+        return _on_stream(stream, tree_gdn_fwd, locals())
     torch = _torch()
     for t in (q, k, v):
         if t.dim() != 3 or t.dtype != torch.bfloat16 or not t.is_contiguous():
@@ -1135,7 +1159,7 @@ def tree_gdn_fwd(q, k, v, g, beta, plan: GdnPlan, *, scale=None, out=None, works
                                   _dp(g), _dp(beta), plan.n_chunks, _dp(d["chunk_tok0"]), _dp(d["chunk_len"]), _dp(d["chunk_src"]),
                                   _dp(d["chunk_dst"]), plan.n_slots, _dp(d["chunk_cap"]) if return_states and plan.n_capture else None,
                                   _sched_ref(plan), _dp(initial_state), _dp(states) if plan.n_capture else None, _dp(out), _dp(workspace), workspace.numel(),
-                                  _stream_ptr(stream)))
+                                  _stream_ptr(None)))
     return (out, states) if return_states else out
 
 
@@ -1152,6 +1176,8 @@ def tree_gdn_bwd(q, k, v, g, beta, d_o, plan: GdnPlan, *, scale=None, initial_st
     bf16, dg, dbeta [n, hv] fp32), plus d_initial_state [hv, 128, 128] fp32 when asked.  d_state_out
     [n_capture, hv, 128, 128] fp32: upstream gradient of the plan's captured end states.  workspace: a uint8 tensor of
     tree_gdn_bwd_workspace(...) bytes (default: allocated here, full size) or of any size down to its `smallest`."""
+    if stream is not None:
+        return _on_stream(stream, tree_gdn_bwd, locals())
     torch = _torch()
     for t in (q, k, v, d_o):
         if t.dim() != 3 or t.dtype != torch.bfloat16 or not t.is_contiguous():
@@ -1182,7 +1208,7 @@ def tree_gdn_bwd(q, k, v, g, beta, d_o, plan: GdnPlan, *, scale=None, initial_st
                                   _dp(g), _dp(beta), _dp(d_o), plan.n_chunks, _dp(d["chunk_tok0"]), _dp(d["chunk_len"]),
                                   _dp(d["chunk_src"]), _dp(d["chunk_dst"]), plan.n_slots, _dp(d["chunk_cap"]) if use_cap else None,
                                   _sched_ref(plan), _dp(initial_state), _dp(d_state_out) if use_cap else None, _dp(dq), _dp(dk_), _dp(dv_), _dp(dg),
-                                  _dp(dbeta), _dp(d_init), _dp(workspace), workspace.numel(), _stream_ptr(stream)))
+                                  _dp(dbeta), _dp(d_init), _dp(workspace), workspace.numel(), _stream_ptr(None)))
     out = (dq, dk_, dv_, dg, dbeta)
     return out + (d_init,) if want_d_initial_state else out
 
