@@ -713,7 +713,7 @@ tt_status tt_tree_gdn_bwd(int64_t n_tokens, int32_t hk, int32_t hv, int32_t dk, 
  *   [channels][n_state] or NULL.  d_state_out: upstream gradient of the captured states, NULL = 0; needs
  *   chunk_cap.  Gradients that several tokens, channels or branches share are summed in fp32 in a fixed
  *   order and rounded once.
- * Outputs may not share memory with inputs.
+ * Outputs may not share memory with inputs (the program among them) or with each other.
  * Alignment: x, dt, z, y, dy and their gradients to the element size; b, c to four elements, with strides
  *   of a multiple of four; fp32 arrays and the workspace to 16 bytes.
  * Errors: TT_ERR_NULL, TT_ERR_SHAPE, TT_ERR_DTYPE, TT_ERR_ALIGN, TT_ERR_UNSUPPORTED (n_state, groups),
@@ -732,6 +732,8 @@ typedef struct {
   const int32_t *chunk_tok0, *chunk_len, *chunk_src, *chunk_dst, *chunk_cap;      /* device */
   const int32_t* chunk_order;       /* device; NULL, or a permutation of the chunks: the order in which they are
                                        started (the longest first, and the last to end are short)             */
+  int32_t n_capture;                /* states that state_out / d_state_out hold: what is checked for sharing memory; 0
+                                       counts as 1                                                            */
 } tt_scan_chunks;
 tt_status tt_tree_scan_program(int32_t n_chunks, const int32_t* chunk_tok0, const int32_t* chunk_len,
                                const int32_t* chunk_src, const int32_t* chunk_dst, const int32_t* chunk_cap,

@@ -324,7 +324,8 @@ class _ScanDesc(ctypes.Structure):
 
 class _ScanChunks(ctypes.Structure):
     _fields_ = [("n_chunks", ctypes.c_int32), ("n_slots", ctypes.c_int32)] + \
-               [(name, _vp) for name in ("chunk_tok0", "chunk_len", "chunk_src", "chunk_dst", "chunk_cap", "chunk_order")]
+               [(name, _vp) for name in ("chunk_tok0", "chunk_len", "chunk_src", "chunk_dst", "chunk_cap", "chunk_order")] + \
+               [("n_capture", ctypes.c_int32)]
 
 
 class _GdnSchedule(ctypes.Structure):
@@ -401,7 +402,7 @@ class GdnPlan:
             packed = _torch().from_numpy(np.concatenate([prog, longest_first[None]])).to(device)
             rows, n = [packed[i].data_ptr() for i in range(6)], prog.shape[1]
             on_device = self.scan_programs[key] = (packed, _ScanChunks(n, self.n_slots, *rows[:4], None, rows[5]),
-                                                   _ScanChunks(n, self.n_slots, *rows), _stream_ptr(None))
+                                                   _ScanChunks(n, self.n_slots, *rows, self.n_capture), _stream_ptr(None))
         if _stream_ptr(None) != on_device[3]:        # not reused, once the plan is dropped, before this stream is through with it
             on_device[0].record_stream(_torch().cuda.current_stream())
         return on_device[2 if captured else 1]

@@ -1,6 +1,7 @@
 // C ABI entry points of the device calls: argument validation on the host, then dispatch to the
 // kernels.  Nothing is launched unless every check passes.
 #include <hip/hip_runtime.h>
+#include <algorithm>
 #include <climits>
 #include <cmath>
 #include <mutex>
@@ -644,6 +645,14 @@ bool meets(const Rows& a, const Rows& b) {
   return shares_memory(a.p, a.step * a.es, a.len * a.es, b.p, b.step * b.es, b.len * b.es, a.n);
 }
 
+// Whether a span lies on an array of the chunk program.
+bool meets_program(const Span& s, const tt_scan_chunks& k) {
+  for (const int32_t* p : {k.chunk_tok0, k.chunk_len, k.chunk_src, k.chunk_dst, k.chunk_cap, k.chunk_order})
+    if (meets(s, Span{p, k.n_chunks * (int64_t)4})) return true;
+  return false;
+}
+int64_t captured(const tt_scan_chunks& k) { return std::max(k.n_capture, 1); }
+
 // Whether one of the outputs (y in rows, a state) lies on an input or on the other.
 bool outputs_meet(const Rows& y, const Span& state, std::initializer_list<Rows> rows, std::initializer_list<Span> whole) {
   for (const Rows& in : rows)
@@ -703,6 +712,7 @@ tt_status check_scan_chunks(const tt_scan_desc& d, const tt_scan_chunks* k) {
   if (k->n_chunks < 0 || k->n_slots < 0) return fail(TT_ERR_SHAPE, "n_chunks=%d, n_slots=%d", k->n_chunks, k->n_slots);
   if ((d.n_tokens > 0) != (k->n_chunks > 0) || k->n_chunks > d.n_tokens || k->n_slots > k->n_chunks)
     return fail(TT_ERR_SHAPE, "n_tokens=%lld with %d chunks and %d saved states", (long long)d.n_tokens, k->n_chunks, k->n_slots);
+  if (k->n_capture < 0 || k->n_capture > k->n_chunks) return fail(TT_ERR_SHAPE, "%d captured states of %d chunks", k->n_capture, k->n_chunks);
   // a dimension of a launch holds less than 2^32 work-items
   if (((int64_t)d.channels + 255) / 256 * k->n_chunks >= 1 << 24 || d.n_tokens * d.groups * d.n_state >= (int64_t)1 << 30)
     return fail(TT_ERR_SHAPE, "%d chunks of %d channels (%d groups of %d states) are more than one launch holds", k->n_chunks, d.channels,
@@ -754,10 +764,13 @@ extern "C" tt_status tt_tree_scan_fwd(const tt_scan_desc* desc, const tt_scan_ch
   if (!aligned_to(y, es)) return fail(TT_ERR_ALIGN, "y is not aligned to its element size");
   if (!tt::aligned16(initial_state) || !tt::aligned16(state_out)) return fail(TT_ERR_ALIGN, "a state is not 16-byte aligned");
   const int64_t bc = (int64_t)d.groups * d.n_state;
-  if (outputs_meet({y, n, d.channels, d.y_stride_tok, es}, {state_out, state_out ? width : 0},
+  const Rows out{y, n, d.channels, d.y_stride_tok, es};
+  const Span states{state_out, state_out ? width * captured(*chunks) : 0};
+  if (outputs_meet(out, states,
                    {{x, n, d.channels, d.x_stride_tok, es}, {dt, n, d.channels, d.dt_stride_tok, es}, {z, n, d.channels, d.z_stride_tok, es},
                     {b, n, bc, d.b_stride_tok, es}, {c, n, bc, d.c_stride_tok, es}},
-                   {{A, width}, {D, d.channels * 4}, {dt_bias, d.channels * 4}, {initial_state, width}}))
+                   {{A, width}, {D, d.channels * 4}, {dt_bias, d.channels * 4}, {initial_state, width}}) ||
+      meets_program(out.span(), *chunks) || meets_program(states, *chunks))
     return fail(TT_ERR_SHAPE, "an output shares memory with another tensor");
   const size_t need = tt::scan_fwd_workspace(d.channels, d.n_state, chunks->n_chunks, chunks->n_slots);
   if (!workspace || workspace_bytes < need || !tt::aligned16(workspace))
@@ -789,12 +802,14 @@ extern "C" tt_status tt_tree_scan_bwd(const tt_scan_desc* desc, const tt_scan_ch
   const Rows ins[] = {{x, n, ch, d.x_stride_tok, es}, {dt, n, ch, d.dt_stride_tok, es}, {z, n, ch, d.z_stride_tok, es},
                       {dy, n, ch, d.y_stride_tok, es}, {b, n, bc, d.b_stride_tok, es}, {c, n, bc, d.c_stride_tok, es},
                       {A, 1, ch * d.n_state, ch * d.n_state, 4}, {D, 1, ch, ch, 4}, {dt_bias, 1, ch, ch, 4},
-                      {initial_state, 1, ch * d.n_state, ch * d.n_state, 4}, {d_state_out, 1, ch * d.n_state, ch * d.n_state, 4}};
+                      {initial_state, 1, ch * d.n_state, ch * d.n_state, 4},
+                      {d_state_out, captured(*chunks), ch * d.n_state, ch * d.n_state, 4}};
   const Span outs[] = {{dx, n * ch * es}, {ddt, n * ch * es}, {dz, n * ch * es}, {db, n * bc * es}, {dc, n * bc * es},
                        {dA, ch * d.n_state * 4}, {dD, ch * 4}, {ddt_bias, ch * 4}, {d_initial_state, ch * d.n_state * 4}};
   for (const Span& o : outs) {
     for (const Rows& i : ins)
       if (meets(o, i.span())) return fail(TT_ERR_SHAPE, "an output shares memory with an input");
+    if (meets_program(o, *chunks)) return fail(TT_ERR_SHAPE, "an output shares memory with the chunk program");
     for (const Span& p : outs)
       if (&p != &o && meets(o, p)) return fail(TT_ERR_SHAPE, "two outputs share memory");
   }

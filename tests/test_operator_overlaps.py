@@ -1,0 +1,55 @@
+"""Outputs that lie on inputs or on other outputs are refused before anything is launched (the pointers are never dereferenced)."""
+import ctypes
+
+from test_operator_refusals import BIG, FAKE, L, P, T, chunks, scan_desc
+
+WIDTH = 128 * 16 * 4                                                    # bytes of a state of scan_desc()
+
+
+def behind(p, n):
+    return P(p.value + n)
+
+
+def test_the_second_captured_state():
+    """state_out and d_state_out hold n_capture states; an overlap with any of them counts."""
+    f = L.tt_tree_scan_fwd
+    ok = dict(x=FAKE[0], dt=FAKE[1], A=FAKE[2], b=FAKE[3], c=FAKE[4], D=FAKE[5], z=FAKE[6], bias=FAKE[7], init=FAKE[8], so=FAKE[11], y=FAKE[9],
+              ws=FAKE[10], wb=BIG)
+
+    def forward(n_capture=2, **a):
+        k = chunks(cap=FAKE[0], slots=2, n=4)
+        k.n_capture = n_capture
+        return f(ctypes.byref(scan_desc()), ctypes.byref(k), *{**ok, **a}.values(), None)
+    for i in range(1, 10):
+        assert forward(so=behind(FAKE[i], -WIDTH)) == -2 and "shares memory" in T.last_error(), i
+        assert forward(n_capture=4, so=behind(FAKE[i], -3 * WIDTH)) == -2 and "shares memory" in T.last_error(), i
+    assert forward(y=behind(FAKE[11], WIDTH)) == -2 and "shares memory" in T.last_error()
+    assert forward(n_capture=-1) == -2 and forward(n_capture=5) == -2 and "captured" in T.last_error()
+    g = L.tt_tree_scan_bwd
+    okb = dict(x=FAKE[0], dt=FAKE[1], A=FAKE[2], b=FAKE[3], c=FAKE[4], D=FAKE[5], z=FAKE[6], bias=FAKE[7], init=FAKE[8], dy=FAKE[9], ds=FAKE[20],
+               dx=FAKE[10], ddt=FAKE[11], dA=FAKE[12], db=FAKE[13], dc=FAKE[14], dD=FAKE[15], dz=FAKE[16], dbias=FAKE[17], dinit=FAKE[18],
+               ws=FAKE[19], wb=BIG)
+
+    def backward(**a):
+        k = chunks(cap=FAKE[0], slots=2, n=4)
+        k.n_capture = 3
+        return g(ctypes.byref(scan_desc()), ctypes.byref(k), *{**okb, **a}.values(), None)
+    for name in ("dx", "ddt", "dA", "db", "dc", "dD", "dz", "dbias", "dinit"):
+        assert backward(**{name: behind(FAKE[20], 2 * WIDTH)}) == -2 and "shares memory" in T.last_error(), name
+
+
+def test_scan_outputs_on_the_chunk_program():
+    f = L.tt_tree_scan_fwd
+    ok = dict(x=FAKE[0], dt=FAKE[1], A=FAKE[2], b=FAKE[3], c=FAKE[4], D=FAKE[5], z=FAKE[6], bias=FAKE[7], init=FAKE[8], so=FAKE[11], y=FAKE[9],
+              ws=FAKE[10], wb=BIG)
+    for i, name in enumerate(("chunk_tok0", "chunk_len", "chunk_src", "chunk_dst", "chunk_cap", "chunk_order")):
+        for out in ("y", "so"):
+            k = chunks(t=FAKE[12], l=FAKE[13], s=FAKE[14], d=FAKE[15], cap=FAKE[16])
+            setattr(k, name, FAKE[17].value)
+            assert f(ctypes.byref(scan_desc()), ctypes.byref(k), *{**ok, out: FAKE[17]}.values(), None) == -2, (name, out)
+            assert "shares memory" in T.last_error()
+    g = L.tt_tree_scan_bwd
+    okb = dict(x=FAKE[0], dt=FAKE[1], A=FAKE[2], b=FAKE[3], c=FAKE[4], D=FAKE[5], z=FAKE[6], bias=FAKE[7], init=FAKE[8], dy=FAKE[9], ds=None,
+               dx=FAKE[10], ddt=FAKE[11], dA=FAKE[12], db=FAKE[13], dc=FAKE[14], dD=FAKE[15], dz=FAKE[16], dbias=FAKE[17], dinit=FAKE[18],
+               ws=FAKE[19], wb=BIG)
+    assert g(ctypes.byref(scan_desc()), ctypes.byref(chunks(s=FAKE[12])), *okb.values(), None) == -2 and "shares memory" in T.last_error()
