@@ -879,6 +879,9 @@ extern "C" tt_status tt_tree_conv_step(int64_t n_rows, int32_t channels, int32_t
   if (meets(out, in) || meets(out.span(), Span{state, n_slots * saved}) || meets(out.span(), Span{state_out, n_rows * saved}) ||
       meets(in.span(), Span{state_out, n_rows * saved}))
     return fail(TT_ERR_SHAPE, "an output shares memory with another tensor");
+  for (const Span& p : {Span{weight, (int64_t)channels * kernel_size * 4}, Span{bias, (int64_t)channels * 4}, Span{index, n_rows * 4}})
+    if (meets(out.span(), p) || meets(Span{state_out, n_rows * saved}, p))
+      return fail(TT_ERR_SHAPE, "an output shares memory with the weight, the bias or the indices");
   tt::ConvStepArgs a{};
   a.n_rows = (int)n_rows; a.channels = channels; a.n_slots = n_slots; a.silu = activation;
   a.x = x; a.state = state; a.x_stride = x_stride_row; a.y_stride = y_stride_row; a.weight = weight; a.bias = bias; a.index = index;

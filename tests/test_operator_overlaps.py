@@ -53,3 +53,13 @@ def test_scan_outputs_on_the_chunk_program():
                dx=FAKE[10], ddt=FAKE[11], dA=FAKE[12], db=FAKE[13], dc=FAKE[14], dD=FAKE[15], dz=FAKE[16], dbias=FAKE[17], dinit=FAKE[18],
                ws=FAKE[19], wb=BIG)
     assert g(ctypes.byref(scan_desc()), ctypes.byref(chunks(s=FAKE[12])), *okb.values(), None) == -2 and "shares memory" in T.last_error()
+
+
+def test_convolution_step():
+    f = L.tt_tree_conv_step
+    ok = dict(n=8, c=64, k=4, dt=0, act=1, x=FAKE[0], xs=0, w=FAKE[1], b=FAKE[2], slots=8, s=FAKE[3], i=FAKE[4], so=FAKE[5], y=FAKE[6], ys=0)
+    call = lambda **a: f(*{**ok, **a}.values(), None)                       # noqa: E731
+    for i, size in ((1, 64 * 4 * 4), (2, 64 * 4), (4, 8 * 4)):              # weight, bias, index: on them, on their last bytes
+        for at in (FAKE[i], behind(FAKE[i], size - 8), behind(FAKE[i], -8)):
+            assert call(y=at) == -2 and "shares memory" in T.last_error(), i
+            assert call(so=at) == -2 and "shares memory" in T.last_error(), i
