@@ -427,6 +427,7 @@ tt_status tt_tree_rope(int64_t n_tokens, int32_t n_heads, int32_t d, int32_t dty
  *   from zero as a whole; those past 5.8e6 are read three times).  Sums are fp32 and their order is fixed.
  *   workspace: tt_tree_logprob_entropy_workspace bytes (few rows are worked on in parts), 16-byte
  *     aligned; 0 from that function means that the sizes are invalid.
+ * Outputs may not share memory with inputs or with each other.
  * Alignment: logits aligned to its element size.
  *
  * tt_tree_logprob_entropy_bwd: gradient of sum_r d_logp_r logp_r + d_entropy_r entropy_r,
@@ -434,7 +435,7 @@ tt_status tt_tree_rope(int64_t n_tokens, int32_t n_heads, int32_t d, int32_t dty
  *   one read of the logits, one write (dtype of the logits, rounded to nearest even).  lse and entropy
  *   are the forward's; d_logp, d_entropy [n_rows] fp32, each may be NULL (= 0).  Ignored rows get
  *   exactly zero (their logits, lse and upstream gradients are not read).  dlogits may be logits when
- *   the strides are equal; otherwise the two may not overlap.  p = exp(z - lse) is off by what lse is rounded by,
+ *   the strides are equal; otherwise it may not overlap an input.  p = exp(z - lse) is off by what lse is rounded by,
  *   at most 2^-13 of it; rows with |lse| of 1024 and more are summed again (slower), and theirs is not.
  * Alignment: both arrays aligned to the element size; where logits and gradient rows are the same
  *   distance from a 16-byte boundary they go in vectors, otherwise element by element.
@@ -458,7 +459,7 @@ tt_status tt_tree_logprob_entropy_bwd(int64_t n_rows, int32_t vocab, int32_t dty
  *   angle_i = axis_pos[pair_axis[i]][t] * theta_base^(-2i/d),  i in [0, d/2)
  * with the rotation of tt_tree_rope (rotate-half pairs, inverse, in place, dtypes, sizes, strides and
  * alignment as there).
- *   n_axes in 1..4; axis_pos [n_axes][n_tokens] int32 (device), any sign; pair_axis [d/2] (HOST, read
+ *   n_axes in 1..4; axis_pos [n_axes][n_tokens] int32 (device; y may not lie on it), any sign; pair_axis [d/2] (HOST, read
  *   during the call), values below n_axes.  With equal positions on all axes the result is that of
  *   tt_tree_rope.
  *

@@ -269,6 +269,25 @@ bool shares_memory(const void* a, int64_t step_a, int64_t len_a, const void* b, 
   return a0 < b1 && b0 < a1;
 }
 
+struct Span { const void* p; int64_t bytes; };
+bool meets(const Span& a, const Span& b) {
+  const uintptr_t a0 = reinterpret_cast<uintptr_t>(a.p), b0 = reinterpret_cast<uintptr_t>(b.p);
+  return a.p && b.p && a.bytes > 0 && b.bytes > 0 && a0 < b0 + (uintptr_t)b.bytes && b0 < a0 + (uintptr_t)a.bytes;
+}
+
+// Rows of `len` elements, `step` apart.
+struct Rows {
+  const void* p;
+  int64_t n, len, step, es;
+  Span span() const { return {p, n > 0 ? ((n - 1) * step + len) * es : 0}; }
+};
+// Whether a span lies on the rows themselves (it may lie between two of them).
+bool meets(const Rows& a, const Span& b) {
+  if (!meets(a.span(), b)) return false;
+  const int64_t off = (int64_t)(reinterpret_cast<uintptr_t>(b.p) - reinterpret_cast<uintptr_t>(a.p)), step = a.step * a.es;
+  return off < 0 || off % step < a.len * a.es || off % step + b.bytes > step;
+}
+
 tt_status check_entropy(int64_t n_rows, int32_t vocab, int32_t dtype) {
   if (dtype != TT_DTYPE_BF16 && dtype != TT_DTYPE_FP32) return fail(TT_ERR_DTYPE, "unknown dtype %d", dtype);
   if (n_rows < 0 || n_rows > 0x7fffffffLL) return fail(TT_ERR_SHAPE, "n_rows=%lld out of range", (long long)n_rows);
@@ -302,6 +321,14 @@ extern "C" tt_status tt_tree_logprob_entropy(int64_t n_rows, int32_t vocab, int3
     return fail(TT_ERR_NULL, "top_index and top_logp must be given exactly when top_k > 0");
   const size_t es = dtype == TT_DTYPE_BF16 ? 2 : 4;
   if (reinterpret_cast<uintptr_t>(logits) % es) return fail(TT_ERR_ALIGN, "logits is not aligned to its element size");
+  const Rows in{logits, n_rows, vocab, row_stride, (int64_t)es};
+  const int64_t top = n_rows * top_k * 4;
+  const Span outs[] = {{logp, n_rows * 4}, {entropy, n_rows * 4}, {lse, n_rows * 4}, {top_index, top}, {top_logp, top}};
+  for (const Span& o : outs) {
+    if (meets(in, o) || meets(o, Span{target, n_rows * 4})) return fail(TT_ERR_SHAPE, "an output shares memory with an input");
+    for (const Span& p : outs)
+      if (&p != &o && meets(o, p)) return fail(TT_ERR_SHAPE, "an output shares memory with another output");
+  }
   const size_t need = tt::logprob_entropy_workspace(n_rows, vocab, dtype == TT_DTYPE_BF16, top_k);
   if (!workspace || workspace_bytes < need || !tt::aligned16(workspace))
     return fail(TT_ERR_WORKSPACE, "tree_logprob_entropy needs %zu bytes of 16-byte aligned workspace, got %zu", need, workspace_bytes);
@@ -328,6 +355,9 @@ extern "C" tt_status tt_tree_logprob_entropy_bwd(int64_t n_rows, int32_t vocab, 
   if (!(dlogits == logits && dlogits_row_stride == row_stride) &&
       shares_memory(logits, row_stride * es, vocab * es, dlogits, dlogits_row_stride * es, vocab * es, n_rows))
     return fail(TT_ERR_SHAPE, "dlogits may share memory with logits only as a whole, with equal row strides");
+  const Rows out{dlogits, n_rows, vocab, dlogits_row_stride, es};
+  for (const void* p : {(const void*)target, (const void*)lse, (const void*)entropy, (const void*)d_logp, (const void*)d_entropy})
+    if (meets(out, Span{p, n_rows * 4})) return fail(TT_ERR_SHAPE, "dlogits shares memory with an input other than the logits");
   return hip_result(tt::logprob_entropy_bwd(n_rows, vocab, dtype == TT_DTYPE_BF16, logits, row_stride, target, lse, entropy, d_logp,
                                             d_entropy, dlogits, dlogits_row_stride, (hipStream_t)stream),
                     "tree_logprob_entropy_bwd");
@@ -358,6 +388,8 @@ extern "C" tt_status tt_tree_rope_axes(int64_t n_tokens, int32_t n_heads, int32_
   const int64_t es = dtype == TT_DTYPE_BF16 ? 2 : 4, len = (int64_t)n_heads * d * es;
   if (!(x == y && x_stride_tok == y_stride_tok) && shares_memory(x, x_stride_tok * es, len, y, y_stride_tok * es, len, n_tokens))
     return fail(TT_ERR_SHAPE, "y may share memory with x only as a whole, with equal token strides");
+  if (meets(Rows{y, n_tokens, (int64_t)n_heads * d, y_stride_tok, es}, Span{axis_pos, n_axes * n_tokens * 4}))
+    return fail(TT_ERR_SHAPE, "y shares memory with axis_pos");
   return hip_result(tt::rope_axes(n_tokens, n_heads, d, dtype == TT_DTYPE_BF16, x, x_stride_tok, axis_pos, pair_axis, theta_base,
                                   inverse != 0, y, y_stride_tok, (hipStream_t)stream),
                     "tree_rope_axes");
@@ -626,18 +658,6 @@ extern "C" tt_status tt_tree_gdn_bwd(int64_t n_tokens, int32_t hk, int32_t hv, i
 
 namespace {
 
-struct Span { const void* p; int64_t bytes; };
-bool meets(const Span& a, const Span& b) {
-  const uintptr_t a0 = reinterpret_cast<uintptr_t>(a.p), b0 = reinterpret_cast<uintptr_t>(b.p);
-  return a.p && b.p && a.bytes > 0 && b.bytes > 0 && a0 < b0 + (uintptr_t)b.bytes && b0 < a0 + (uintptr_t)a.bytes;
-}
-
-// Rows of `len` elements, `step` apart.
-struct Rows {
-  const void* p;
-  int64_t n, len, step, es;
-  Span span() const { return {p, n > 0 ? ((n - 1) * step + len) * es : 0}; }
-};
 // Whether an output lies on an input: exact for rows of equal step (slices of one buffer), by their extents otherwise.
 bool meets(const Rows& a, const Rows& b) {
   if (!a.p || !b.p || a.n <= 0 || b.n <= 0) return false;

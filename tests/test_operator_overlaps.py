@@ -63,3 +63,29 @@ def test_convolution_step():
         for at in (FAKE[i], behind(FAKE[i], size - 8), behind(FAKE[i], -8)):
             assert call(y=at) == -2 and "shares memory" in T.last_error(), i
             assert call(so=at) == -2 and "shares memory" in T.last_error(), i
+
+
+def test_logprob_entropy():
+    """Outputs on the logits, the targets, or each other; the gradient on the per-row inputs."""
+    f = L.tt_tree_logprob_entropy
+    n, v, k = 4, 128, 5
+    ok = dict(n=n, v=v, dt=0, z=FAKE[0], zs=0, y=FAKE[1], k=k, logp=FAKE[2], ent=FAKE[3], lse=FAKE[4], ti=FAKE[5], tl=FAKE[6], ws=FAKE[7], wb=BIG)
+    call = lambda **a: f(*{**ok, **a}.values(), None)                       # noqa: E731
+    outs = {"logp": n * 4, "ent": n * 4, "lse": n * 4, "ti": n * k * 4, "tl": n * k * 4}
+    for name, size in outs.items():
+        for at in (behind(FAKE[0], n * v * 2 - 4), FAKE[1], behind(FAKE[1], 4 - size), behind(FAKE[0], 4 - size)):
+            assert call(**{name: at}) == -2 and "shares memory" in T.last_error(), name
+        for other in outs:
+            if other != name:
+                assert call(**{name: behind(ok[other], 4 - size)}) == -2 and "shares memory" in T.last_error(), (name, other)
+    g = L.tt_tree_logprob_entropy_bwd
+    ok = dict(n=n, v=v, dt=1, z=FAKE[0], zs=0, y=FAKE[1], lse=FAKE[2], ent=FAKE[3], a=FAKE[5], b=FAKE[6], out=FAKE[4], os=0)
+    for name in ("y", "lse", "ent", "a", "b"):
+        for at in (FAKE[4], behind(FAKE[4], n * v * 4 - 4), behind(FAKE[4], 4 - n * 4)):
+            assert g(*{**ok, name: at}.values(), None) == -2 and "shares memory" in T.last_error(), name
+
+
+def test_rotation_on_its_positions():
+    ok = dict(n=4, h=4, d=128, dt=0, x=FAKE[0], xs=0, na=3, pos=FAKE[1], map=bytes(64), base=1e6, inv=0, y=FAKE[2], ys=0)
+    for at in (FAKE[2], behind(FAKE[2], 4 * 512 * 2 - 4), behind(FAKE[2], 4 - 3 * 4 * 4)):
+        assert L.tt_tree_rope_axes(*{**ok, "pos": at}.values(), None) == -2 and "shares memory" in T.last_error()
