@@ -612,6 +612,9 @@ def _workspace(desc, backward, workspace, device):
     return workspace, workspace.numel() * workspace.element_size()
 
 
+I32_MAX = 2 ** 31 - 1        # what the library's sizes hold (ctypes would pass the lower bits of a larger one)
+
+
 def _check_tensor(t, name, shape, dtype):
     """A contiguous tensor of exactly this shape and dtype."""
     if t.shape != shape or t.dtype is not dtype or not t.is_contiguous():
@@ -622,8 +625,11 @@ def _check_rows(t, name, shape, dtypes):
     """Rows of contiguous elements with a free stride between them (one of the dtypes); returns that stride in elements."""
     if t.shape != shape or t.dtype not in dtypes:
         raise ValueError(f"{name} must be {shape} of {' / '.join(str(d) for d in dtypes)}")
+    width = shape[1] if len(shape) == 2 else shape[1] * shape[2]
+    if width > I32_MAX:
+        raise ValueError(f"the rows of {name} hold at most {I32_MAX} elements, not {width}")
     if t.is_contiguous():
-        return shape[1] if len(shape) == 2 else shape[1] * shape[2]
+        return width
     step = t.stride()
     row = 1
     for i in range(len(shape) - 1, 0, -1):
@@ -631,8 +637,8 @@ def _check_rows(t, name, shape, dtypes):
             raise ValueError(f"the rows of {name} must be contiguous (only the stride between them is free)")
         row *= shape[i]
     if shape[0] <= 1:
-        return row
-    if step[0] < row:
+        return width
+    if step[0] < width:
         raise ValueError(f"the rows of {name} overlap")
     return step[0]
 
@@ -849,15 +855,22 @@ def _logits_dtype(logits) -> int:
     torch = _torch()
     if logits.dim() != 2:
         raise ValueError("logits must be [rows, vocab]")
+    if logits.dtype not in (torch.bfloat16, torch.float32):
+        raise ValueError("logits must be bf16 or fp32")
     return DTYPE_BF16 if logits.dtype == torch.bfloat16 else DTYPE_FP32
 
 
 def tree_logprob_entropy_workspace(logits, top_k: int = 0) -> int:
     """Bytes of workspace of tree_logprob_entropy for these logits."""
     code, (n, vocab) = _logits_dtype(logits), logits.shape
-    need = int(_lib().tt_tree_logprob_entropy_workspace(n, vocab, code, int(top_k)))
+    return _logprob_entropy_workspace(n, vocab, code, top_k)
+
+
+def _logprob_entropy_workspace(n, vocab, code, top_k) -> int:
+    small = 0 <= top_k <= LOGPROB_TOP_MAX and vocab <= I32_MAX
+    need = _lib().tt_tree_logprob_entropy_workspace(n, vocab, code, int(top_k)) if small else 0
     if need == 0:
-        raise ValueError(f"top_k={top_k} must lie in [0, min({LOGPROB_TOP_MAX}, vocab={vocab})]")
+        raise ValueError(f"top_k={top_k} must lie in [0, min({LOGPROB_TOP_MAX}, vocab={vocab})], and the vocabulary in [1, 2^30]")
     return need
 
 
@@ -874,7 +887,7 @@ def tree_logprob_entropy(logits, target, *, top_k: int = 0, logp=None, entropy=N
     stride = _check_rows(logits, "logits", (n, vocab), (torch.bfloat16, torch.float32))
     _check_tensor(target, "target", (n,), torch.int32)
     top_k = int(top_k)
-    need = tree_logprob_entropy_workspace(logits, top_k) if n else 256
+    need = _logprob_entropy_workspace(n, vocab, code, top_k)
     for name, t in (("logp", logp), ("entropy", entropy), ("lse", lse)):
         if t is not None:
             _check_tensor(t, name, (n,), torch.float32)
@@ -1291,10 +1304,12 @@ def tree_scan_fwd(x, dt, A, B, C, plan: GdnPlan, *, D=None, z=None, dt_bias=None
 
 def tree_scan_workspace(x, A, B, plan: GdnPlan, backward: bool = False) -> int:
     """Bytes of workspace of tree_scan_fwd or tree_scan_bwd for tensors of these shapes."""
-    torch = _torch()
-    desc = _ScanDesc(x.shape[0], x.shape[1], A.shape[1], B.shape[1], DTYPE_BF16 if x.dtype == torch.bfloat16 else DTYPE_FP32, 1)
+    desc = _scan_desc(x, x, A, B, B, None, None, None, True)
     f = _lib().tt_tree_scan_bwd_workspace if backward else _lib().tt_tree_scan_fwd_workspace
-    return int(f(ctypes.byref(desc), plan._scan_program(x.shape[1], backward).shape[1], plan.n_slots))
+    need = int(f(ctypes.byref(desc), plan._scan_program(desc.channels, backward).shape[1], plan.n_slots))
+    if need == 0:
+        raise ValueError(f"sizes must lie in what the scan is built for: {last_error()}")
+    return need
 
 
 def tree_scan_bwd(x, dt, A, B, C, d_y, plan: GdnPlan, *, D=None, z=None, dt_bias=None, softplus: bool = True, initial_state=None,
@@ -1344,6 +1359,8 @@ def tree_scan_step(x, dt, A, B, C, state, *, index=None, D=None, z=None, dt_bias
     desc = _scan_desc(x, dt, A, B, C, D, z, dt_bias, softplus)
     n, ch, m = desc.n_tokens, desc.channels, desc.n_state
     slots = state.shape[0]
+    if slots > I32_MAX:
+        raise ValueError(f"at most {I32_MAX} slots, not {slots}")
     _check_tensor(state, "state", (slots, ch, m), torch.float32)
     if index is not None:
         _check_tensor(index, "index", (n,), torch.int32)
@@ -1376,6 +1393,8 @@ def tree_conv_step(x, state, weight, bias=None, *, index=None, silu: bool = True
     k = weight.shape[1]
     xs = _check_rows(x, "x", (n, c), (torch.bfloat16, torch.float32))
     slots = state.shape[0]
+    if slots > I32_MAX or k > I32_MAX:
+        raise ValueError(f"at most {I32_MAX} slots, not {slots}, and taps, not {k}")
     _check_tensor(state, "state", (slots, k - 1, c), x.dtype)
     _check_tensor(weight, "weight", (c, k), torch.float32)
     if bias is not None:
