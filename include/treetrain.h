@@ -765,7 +765,7 @@ tt_status tt_tree_scan_bwd(const tt_scan_desc* desc, const tt_scan_chunks* chunk
  *   [n_slots][channels][n_state], state_out [n_tokens][channels][n_state], fp32.
  * tt_tree_conv_step: x, y [n_rows][channels] (row strides in elements, 0 = channels), weight, bias, activation
  *   as for tt_tree_conv_fwd; state [n_slots][K-1][channels], state_out [n_rows][K-1][channels] in the dtype of
- *   x: the inputs before the token, the oldest first.  channels a multiple of 4.
+ *   x: the inputs before the token, the oldest first.  channels a multiple of 4, at most 2^30.
  * state_out may be state itself when index is NULL (in place); otherwise outputs may not share memory with
  * inputs.
  * Alignment: as for the scan; the convolution's pointers and rows to four elements, fp32 arrays to 4 bytes.

@@ -881,7 +881,8 @@ extern "C" tt_status tt_tree_conv_step(int64_t n_rows, int32_t channels, int32_t
   if (n_rows < 0 || n_rows >= INT32_MAX) return fail(TT_ERR_SHAPE, "n_rows=%lld out of range", (long long)n_rows);
   if (kernel_size < 2 || kernel_size > 4) return fail(TT_ERR_UNSUPPORTED, "kernel_size=%d: only 2, 3, 4 are built", kernel_size);
   if (activation != 0 && activation != 1) return fail(TT_ERR_UNSUPPORTED, "activation=%d: 0 (none) or 1 (SiLU)", activation);
-  if (channels <= 0 || channels % 4) return fail(TT_ERR_SHAPE, "channels=%d must be a positive multiple of 4", channels);
+  if (channels <= 0 || channels % 4 || channels > 1 << 30)
+    return fail(TT_ERR_SHAPE, "channels=%d must be a positive multiple of 4, at most 2^30", channels);
   if (x_stride_row == 0) x_stride_row = channels;
   if (y_stride_row == 0) y_stride_row = channels;
   if (x_stride_row < channels || y_stride_row < channels || x_stride_row % 4 || y_stride_row % 4)

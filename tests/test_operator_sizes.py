@@ -4,6 +4,7 @@ import pytest
 import torch
 
 import paper_2511_00413_amd as T
+from test_operator_refusals import FAKE, L
 
 F32 = torch.float32
 WRAP = 1 << 32
@@ -46,3 +47,9 @@ def test_workspace_of_types_that_are_not_built():
         T.tree_scan_workspace(torch.zeros(2, 64), torch.zeros(64, 5), torch.zeros(2, 1, 5), plan)
     assert T.tree_scan_workspace(torch.zeros(2, 64), torch.zeros(64, 4), torch.zeros(2, 1, 4), plan) > 0
     assert T.tree_scan_workspace(torch.zeros(0, 64), torch.zeros(64, 4), torch.zeros(0, 1, 4), T.tree_gdn_plan([-1], [0]), backward=True) > 0
+
+
+def test_channels_of_a_convolution_step():
+    """The last workgroup's channels reach past 2^31 from 2^31 - 1020 on."""
+    ok = dict(n=1, c=(1 << 31) - 512, k=2, dt=0, act=1, x=FAKE[0], xs=0, w=FAKE[1], b=None, slots=1, s=FAKE[3], i=None, so=FAKE[5], y=FAKE[6], ys=0)
+    assert L.tt_tree_conv_step(*ok.values(), None) == -2 and "channels" in T.last_error()
