@@ -341,7 +341,8 @@ def _sched_ref(plan):
 
 @dataclass
 class GdnPlan:
-    """Host output of tt_tree_gdn_plan: the chunk program of the gated-delta-rule scan."""
+    """Host output of tt_tree_gdn_plan: the chunk program of the gated delta rule and of the selective scan.  The device calls read copies of it
+    that belong to the plan: a graph that holds such a call needs the plan as long as it is replayed."""
     n_chunks: int
     n_slots: int
     chunk_tok0: np.ndarray
@@ -1275,8 +1276,8 @@ def tree_scan_fwd(x, dt, A, B, C, plan: GdnPlan, *, D=None, z=None, dt_bias=None
                   return_states: bool = False, out=None, workspace=None, stream=None):
     """Selective state space scan with tree state routing: x, dt [n, channels], B, C [n, groups, states] bf16 or fp32 (free token
     strides), A [channels, states] fp32 (negative), D, dt_bias [channels] fp32 or None, z [n, channels] (the gate) or None; the
-    chunk program is tree_gdn_plan's, whose first call with these many channels copies it to the device (so not one that a graph
-    captures).  Returns y [n, channels]; with return_states also the end states [n_capture, channels, states] fp32 of the plan's
+    chunk program is tree_gdn_plan's, whose first call with these many channels lays it out and copies it to the device (so not one that
+    a graph captures; the graph needs the plan afterwards).  Returns y [n, channels]; with return_states also the end states [n_capture, channels, states] fp32 of the plan's
     capture nodes.  initial_state [channels, states] fp32: the state every root starts from."""
     if stream is not None:
         return _on_stream(stream, tree_scan_fwd, locals())

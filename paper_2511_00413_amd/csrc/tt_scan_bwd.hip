@@ -122,7 +122,7 @@ scan_bwd_states_kernel(ScanArgs a, float* local, float* back, const float* __res
   walk<true>(a, back, steps, w, a2, a.d_state_out != nullptr, [&](const Entries& e, const float (&decay)[WALK], const float (&own)[WALK],
                                                                   float (&leaving)[WALK]) {
     const uint32_t continued = mask_of(e.src_behind == -2), saves = mask_of(e.dst >= 0), captured = mask_of(e.cap >= 0);
-    const uint32_t used = continued | saves | captured;                        // (steps are not there where no state is used)
+    const uint32_t used = continued | saves | captured;        // (elsewhere g is 0, and steps as given below 0 may make the decay infinite)
     const uint32_t starts = mask_of(e.src != -2);
     const int to = e.src < 0 ? slots.first : e.src;
     float given[WALK];
