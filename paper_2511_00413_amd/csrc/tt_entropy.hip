@@ -173,24 +173,46 @@ struct Result {
   }
 };
 
-// The sums of a row of extreme logits against its maximum, differences taken before they are scaled: two more passes.  A barrier lies
-// behind the last read of the row.
+// f(z) for a thread's entries of a row: whole vectors, four in flight, behind a scalar head.
+template <typename T, typename F>
+__device__ __forceinline__ void each_entry(const T* row, int vocab, F f) {
+  constexpr int EPV = Row<T>::EPV;
+  const int t = threadIdx.x;
+  const int head = min((int)(((16 - (reinterpret_cast<uintptr_t>(row) & 15)) & 15) / sizeof(T)), vocab), nvec = (vocab - head) / EPV;
+  const u32x4* vp = reinterpret_cast<const u32x4*>(row + head);
+  auto vec = [&](const u32x4& v) {
+    float z[EPV];
+    Row<T>::unpack(v, z);
+#pragma unroll
+    for (int e = 0; e < EPV; e++) f(z[e]);
+  };
+  for (int e = t; e < head; e += THREADS) f(Row<T>::at(row, e));
+  int i = t;
+  for (; i + 3 * THREADS < nvec; i += 4 * THREADS) {
+    const u32x4 a = vp[i], b = vp[i + THREADS], c = vp[i + 2 * THREADS], d = vp[i + 3 * THREADS];
+    vec(a); vec(b); vec(c); vec(d);
+  }
+  for (; i < nvec; i += THREADS) vec(vp[i]);
+  for (int e = head + nvec * EPV + t; e < vocab; e += THREADS) f(Row<T>::at(row, e));
+}
+
+// The sums of a row of extreme logits against its maximum, differences taken before they are scaled: two more passes.
 template <typename T>
 __device__ Result far_row(Stat (&part)[WAVES], const T* row, int vocab) {
   const int t = threadIdx.x;
   float m = -INFINITY;
-  for (int e = t; e < vocab; e += THREADS) m = fmaxf(m, Row<T>::at(row, e));
+  each_entry(row, vocab, [&](float z) { m = fmaxf(m, z); });
   m = wave_all(m, [](float a, float b) { return fmaxf(a, b); });
   __syncthreads();                           // (the sums in part have been read)
   if ((t & 63) == 0) part[t >> 6].r = m;
   __syncthreads();
   for (int w = 0; w < WAVES; w++) m = fmaxf(m, part[w].r);
   Stat st = {0.f, 0.f, 0.f};
-  for (int e = t; e < vocab; e += THREADS) {
-    const float d = Row<T>::at(row, e) - m, p = ex2(d * LOG2E);
+  each_entry(row, vocab, [&](float z) {
+    const float d = z - m, p = ex2(d * LOG2E);
     st.s += p;
     st.u = fmaf(p, fmaxf(d, FAR), st.u);
-  }
+  });
   __syncthreads();
   st = join(part, st);
   const float ln_s = LN2 * log2f(st.s);
@@ -479,8 +501,10 @@ entropy_join_kernel(int64_t row0, int vocab, const T* __restrict__ logits, int64
 // A row is cut into parts of 16 KB, one workgroup each, four vectors in flight per thread.
 // Gradient and logits rows the same distance from a 16-byte boundary go in vectors behind a scalar head.
 // p = exp(z - lse) is off by what lse is rounded by, some |lse| 2^-23: 10^-4 of it at SUM_AGAIN (a twentieth of half a step in bf16), all
-// of it where ln s does not reach lse's last digit.  Rows from there on, which no trained model has, and rows without a distribution are
-// summed again by the workgroup of their first part, which then takes the whole row.
+// of it where ln s does not reach lse's last digit.  In rows from there on, which no trained model has, and rows without a distribution
+// the workgroup of one part adds up p once more and takes the whole row: lse lies within 33 of the exact one (half its last digit,
+// or, where ln s does not reach that, ln s itself), so the sum stays in range, and its logarithm is what lse is off by.  4096 rows of
+// 32003 in fp32: 242 us instead of 189 (their forward, three reads, 234 instead of 87).
 constexpr float SUM_AGAIN = 1024.f;
 template <typename T>
 __global__ void __launch_bounds__(THREADS)
@@ -489,7 +513,7 @@ entropy_bwd_kernel(int64_t row0, int vocab, const T* logits, int64_t row_stride,
                    const float* __restrict__ d_entropy, T* dlogits, int64_t out_stride, int parts, int part_vecs) {
   constexpr int EPV = Row<T>::EPV;
   const int64_t r = row0 + (int64_t)(blockIdx.x / (unsigned)parts);
-  const int part = (int)(blockIdx.x % (unsigned)parts);
+  int part = (int)(blockIdx.x % (unsigned)parts);
   const T* row = logits + r * row_stride;
   T* out = dlogits + r * out_stride;
   const int t = threadIdx.x;
@@ -499,14 +523,14 @@ entropy_bwd_kernel(int64_t row0, int vocab, const T* logits, int64_t row_stride,
   const float lse = used ? lse_in[r] : 0.f;
   const float c = a + b * (used ? entropy[r] : 0.f);
   __shared__ Stat sums[WAVES];
+  float off = 0.f;                          // what lse is off by
   if (used && !(fabsf(lse) < SUM_AGAIN)) {
-    if (part > 0) return;
-    const Result res = far_row(sums, row, vocab);
-    for (int e = t; e < vocab; e += THREADS) {
-      const float d = res.logp(Row<T>::at(row, e));
-      Row<T>::put(out, e, -ex2(d * LOG2E) * fmaf(b, fmaxf(d, FAR), c) + (e == y ? a : 0.f));
-    }
-    return;
+    if (part != (int)(r / 8 % parts)) return;               // (workgroups go round the eight XCDs: always the same part may be one of them)
+    float s = 0.f;
+    each_entry(row, vocab, [&](float z) { s += ex2((z - lse) * LOG2E); });
+    off = LN2 * log2f(join(sums, {0.f, s, 0.f}).s);           // (the barrier in join: the row may be written from here on)
+    part = 0;
+    parts = 1;
   }
   const bool vec_ok = ((reinterpret_cast<uintptr_t>(row) ^ reinterpret_cast<uintptr_t>(out)) & 15) == 0;
   const int head = vec_ok ? min((int)(((16 - (reinterpret_cast<uintptr_t>(row) & 15)) & 15) / sizeof(T)), vocab) : 0;
@@ -515,7 +539,7 @@ entropy_bwd_kernel(int64_t row0, int vocab, const T* logits, int64_t row_stride,
   u32x4* op = reinterpret_cast<u32x4*>(out + head);
   // -p (a + b (ln p + entropy)); far below the maximum p is 0 and the cut keeps the other factor finite
   auto grad1 = [&](float z) {
-    const float d = z - lse;
+    const float d = (z - lse) - off;
     return -ex2(d * LOG2E) * fmaf(b, fmaxf(d, FAR), c);
   };
   auto grad = [&](const u32x4& v, int i) {
