@@ -14,9 +14,9 @@
 // above the complement of the index -- so no two are equal, ties go to the lowest index, and the order in which candidates are
 // collected does not matter.  Where more candidates tie at the bound than the list holds, the row is read again once per alternative.
 //
-// Bound by HBM, every logit being read once: 4096 rows of 151936 in bf16 198 us (6.3 TB/s), their gradient 404 us (6.2 TB/s).  With
-// alternatives the vector ALU is 86 % busy: 8191 rows of 32003, five, 107 us (4.9 TB/s).  Few rows are cut into parts for one workgroup
-// each, joined by a second launch.
+// Bound by HBM, every logit being read once: 4096 rows of 151936 in bf16 188 us (6.6 TB/s), their gradient 400 us (6.2 TB/s).  With
+// alternatives the vector ALU is 89 % busy: 8191 rows of 32003, five, 103 us (5.1 TB/s; 125 some milliseconds into passes without a
+// pause, when the clock is lower).  Few rows are cut into parts for one workgroup each, joined by a second launch.
 #include <hip/hip_runtime.h>
 #include <algorithm>
 #include <type_traits>

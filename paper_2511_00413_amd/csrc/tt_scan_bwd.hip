@@ -15,7 +15,8 @@
 // No atomics: every sum has a fixed order.  One lane holds one channel; the sums over a wave's 64 channels for the 2 NS entries of
 // dB and dC are taken together, the lanes halving the entries they keep at every step (70 instructions for 32 sums).
 //
-// Bound by the vector ALU, as the forward: 16406 tokens of 4096 channels, ends 285 us (106 % busy), states 61, grads 961 (87 %), sums 31.
+// Bound by the vector ALU, as the forward: 16406 tokens of 4096 channels, ends 260 us (105 % busy), states 65, grads 877 (87 %), sums 32
+// (1234 of a pass of 1238).  In fp32, where grads spills 26 registers at 16 gated states, the pass takes 1598.
 #include <algorithm>
 #include "tt_scan.h"
 
@@ -412,7 +413,7 @@ size_t up(size_t v) { return (v + 255) & ~(size_t)255; }
 
 // Strips of chunks that one wave per channel block takes one after the other, keeping dA in registers: as many as give the chip
 // 6144 waves, three times what it holds at a time (2048 / 4096 / 6144 / 8192 waves and one chunk each, with the sums over the strips,
-// 16406 tokens of 4096 channels: 1014 / 1004 / 946 / 998 / 983 us).
+// 16406 tokens of 4096 channels, first passes after a pause: 1014 / 1004 / 946 / 998 / 983 us).
 int strips_of(int channels, int n_chunks) {
   const int blocks = (channels + WAVE - 1) / WAVE;
   return std::max(1, std::min(n_chunks, (6144 + blocks - 1) / blocks));
