@@ -9,7 +9,7 @@ from __future__ import annotations
 import ctypes
 import functools
 import os
-from dataclasses import dataclass, field
+from dataclasses import dataclass
 from typing import NamedTuple, Optional
 
 import numpy as np
@@ -359,8 +359,7 @@ class GdnPlan:
     slot_cons_off: Optional[np.ndarray] = None
     slot_cons: Optional[np.ndarray] = None
     parallel: bool = True          # False: the device calls walk all chunks in sequence order (for cross-checks)
-    # the scan's programs, by channels and direction, on the host and on devices; a copy of the plan has its own
-    scan_programs: Optional[dict] = field(default=None, init=False, repr=False, compare=False)
+    scan_programs = None           # (no field) the scan's programs, by channels and direction, on the host and on devices; a copy has its own
 
     def __getstate__(self):
         return {**self.__dict__, "scan_programs": None}

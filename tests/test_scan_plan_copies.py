@@ -31,3 +31,8 @@ def test_a_changed_plan_is_laid_out_anew():
     other = dataclasses.replace(plan, chunk_cap=want.chunk_cap)
     assert np.array_equal(other._scan_program(64, False), want._scan_program(64, False))
     assert not np.array_equal(other._scan_program(64, False), plan._scan_program(64, False))
+
+
+def test_the_fields_of_a_used_plan():
+    plan = used_plan()
+    assert dataclasses.asdict(plan).keys() == dataclasses.asdict(T.tree_gdn_plan([-1], [3])).keys() and "scan" not in repr(plan)
